@@ -371,6 +371,58 @@ int isc_debug_residual_form(int32_t res_mult, int32_t res_shift, int32_t zp_res,
 int isc_set_option(isc_model *m, const char *name, int64_t value);
 int isc_get_info(isc_model *m, const char *name, int64_t *out);
 
+/*
+ * Operators on device tensors: the answer end of a quantised language model, for Monte-Carlo loops (or plain serving)
+ * whose base classifier is one.  (The paper has no counterpart; its networks are the layer lists above.)  The rows of a
+ * call are tokens or noisy copies: isc_rms_norm_quant closes the residual stream and hands on int8 rows,
+ * isc_quant_linear multiplies them with an int8 matrix (the vocabulary's, or any projection's) beside the low-rank
+ * adapters of the rows' requests, and isc_log_probs turns logits, these or a layer list's int8 ones, into log
+ * probabilities, entropies, alternatives and the votes that isc_decide_predict and isc_decide_certify decide on.
+ *
+ * Unlike the calls above, these take DEVICE pointers, only enqueue work on `cuda_stream` and return at once; they
+ * allocate nothing, keep nothing from call to call and may be captured into a graph.  The device that the pointers
+ * belong to has to be the current one.  Calls may overlap in time as long as no two share a work space.  Tensors are
+ * row-major with a row pitch (ld...) in elements and adjacent elements within a row; outputs may not overlap inputs
+ * where nothing else is said.  Calls with zero rows do nothing.  Element types:
+ */
+typedef enum { ISC_BF16 = 0, ISC_F16 = 1, ISC_F32 = 2, ISC_I8 = 3 } isc_type;
+
+/*
+ * isc_rms_norm_quant -- root-mean-square norm of x + residual, as int8 rows with a scale each:
+ *   h = x + residual,  p_i = h_i * weight_i,  scale = max |p| / sqrt(mean(h^2) + eps) / 127,
+ *   q_i = p_i * 127 / max |p| rounded to the nearest integer (ties to even), so that q_i * scale is the normed value.
+ * h is not rounded before it is normed.  The codes are those of the exact quotient (evaluated in double precision where
+ * single precision leaves a doubt).
+ *   x, residual : [rows][width] of `type` (ISC_BF16, ISC_F16, ISC_F32); residual NULL = none.
+ *   weight      : [width] of `weight_type`: `type` or ISC_F32.       eps >= 0.
+ *   sum         : [rows][width] of `type`, receives h rounded to it, or NULL; may be x or residual itself.
+ *   q           : [rows][width] int8, pitch ldq (a multiple of 16 for isc_quant_linear; bytes behind the row's end are
+ *                 left as they are).      scale : [rows].
+ * A row of zeros has scale 0 and codes 0; a row with an infinity or NaN in h or p has scale NaN and codes 0.
+ * Errors: ISC_ERR_ARG, ISC_ERR_UNSUPPORTED (2^31 rows or elements of a row and more), ISC_ERR_CUDA.
+ */
+int isc_rms_norm_quant(const void *x, int64_t ldx, const void *residual, int64_t ldr, const void *weight, int weight_type,
+                       int type, int64_t rows, int64_t width, float eps, void *sum, int64_t lds, int8_t *q, int64_t ldq,
+                       float *scale, void *cuda_stream);
+
+/*
+ * isc_log_probs -- per row of logits l, with z_i = scale * (l_i - max l) and S = sum exp(z):
+ *   out_log_probs : [rows]  z_target - log S; 0 where the target is negative, NaN where it is `vocab` or more.
+ *   out_entropy   : [rows]  log S - sum(exp(z_i) z_i) / S, in nats.
+ *   out_top_ids, out_top_log_probs : [rows][top]  the `top` tokens of the largest logits in falling order, ties to the
+ *                   lowest index, and their log probabilities.
+ *   votes         : [vocab] int32; 1 is added to the entry of each row's first token.
+ *   logits : [rows][vocab] of `type`, any isc_type.   targets : [rows] int64.   0 <= top <= 32.   scale > 0 (the inverse
+ *   temperature).  Any of targets (with out_log_probs), out_entropy, votes may be NULL, out_top_* only with top = 0.
+ * A logit of minus infinity is masked: probability 0, never an alternative.  Where a row has fewer than `top` others, the
+ * rest of its alternatives has id -1 and log probability -inf.  A row with nothing but masks has log probability -inf,
+ * entropy 0 and no vote.  A row with a NaN or plus infinity has NaN results, ids -1 and no vote.
+ * Sums are held in single precision.  Errors: ISC_ERR_ARG, ISC_ERR_UNSUPPORTED (2^31 rows or columns), ISC_ERR_CUDA.
+ */
+int isc_log_probs(const void *logits, int64_t ld, int type, int64_t rows, int64_t vocab, float scale,
+                  const int64_t *targets, int top, float *out_log_probs, float *out_entropy, int32_t *out_top_ids,
+                  float *out_top_log_probs, int32_t *votes, void *cuda_stream);
+
 const char *isc_strerror(int code);
 
 #ifdef __cplusplus

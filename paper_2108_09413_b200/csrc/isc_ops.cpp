@@ -1,0 +1,46 @@
+// Host part that the operators on device tensors share.
+#include "isc_ops.h"
+
+#include <atomic>
+#include <cstdio>
+#include <cstdlib>
+
+namespace isc {
+namespace ops {
+
+cudaError_t current_device(Device *out)
+{
+    constexpr int kMost = 64;
+    static std::atomic<int> sms[kMost];
+    static std::atomic<void *> encoder[kMost];
+    int ordinal = 0;
+    cudaError_t e = cudaGetDevice(&ordinal);
+    if (e != cudaSuccess) return e;
+    const int slot = ordinal < kMost ? ordinal : kMost - 1;
+    int n = ordinal < kMost ? sms[slot].load(std::memory_order_acquire) : 0;
+    void *fn = encoder[slot].load(std::memory_order_acquire);
+    if (!n) {
+        e = cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, ordinal);
+        if (e != cudaSuccess) return e;
+        cudaDriverEntryPointQueryResult qr;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &qr) != cudaSuccess || qr != cudaDriverEntryPointSuccess) {
+            fn = nullptr;
+            cudaGetLastError();
+        }
+        encoder[slot].store(fn, std::memory_order_release);
+        if (ordinal < kMost) sms[slot].store(n, std::memory_order_release);
+    }
+    *out = Device{ordinal, n, fn};
+    return cudaSuccess;
+}
+
+int status_of(cudaError_t e, const char *what)
+{
+    if (e == cudaSuccess) return ISC_OK;
+    if (getenv("ISC_DEBUG_CUDA")) fprintf(stderr, "isc: %s: %s\n", what, cudaGetErrorString(e));
+    cudaGetLastError();
+    return e == cudaErrorMemoryAllocation ? ISC_ERR_NOMEM : ISC_ERR_CUDA;
+}
+
+}  // namespace ops
+}  // namespace isc
