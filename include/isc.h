@@ -423,6 +423,13 @@ int isc_log_probs(const void *logits, int64_t ld, int type, int64_t rows, int64_
                   const int64_t *targets, int top, float *out_log_probs, float *out_entropy, int32_t *out_top_ids,
                   float *out_top_log_probs, int32_t *votes, void *cuda_stream);
 
+/*
+ * isc_operator_status -- waits for `cuda_stream` and tells whether a bounded wait of an operator's kernel has run out on the
+ * current device since the last call (its rows' scales or results are NaN then).  Not to be captured.
+ * Returns ISC_OK, ISC_ERR_TIMEOUT, or ISC_ERR_CUDA when the stream's work failed.
+ */
+int isc_operator_status(void *cuda_stream);
+
 const char *isc_strerror(int code);
 
 #ifdef __cplusplus

@@ -6,8 +6,8 @@
 // codes need no second reduction.  A row is read once and stays in registers: as it lies in memory, because the codes near a
 // border between two are computed again from it.
 //
-// The codes are those of the exact quotient.  In single precision v = p * (127 / max |p|) is off by at most six roundings,
-// |v| 2^-21.4; where v is nearer than |v| 2^-21 to the middle between two codes, p and max |p| are computed in double
+// The codes are those of the exact quotient.  In single precision v = p * (127 / max |p|) is off by at most seven roundings,
+// |v| 2^-21.2; where v is nearer than |v| 2^-21 to the middle between two codes, p and max |p| are computed in double
 // precision and divided there.  One row in ten of 4,096 elements has such a code.  Rows whose sums leave the range of single
 // precision (values above 1e19 or all below 1e-15, zeros, infinities, NaN) are computed in double precision altogether.
 //
@@ -27,8 +27,10 @@ namespace {
 
 using namespace ops;
 
-constexpr int kChunks = 4;              // chunks of eight elements a thread holds
-constexpr int kBlock = 512;             // most threads for a row
+__device__ int timeout_word;            // not zero: a bounded wait has run out
+
+constexpr int kChunks = 2;              // chunks of eight elements a thread holds
+constexpr int kBlock = 1024;            // most threads for a row
 constexpr int kHeld = kBlock * kChunks * 8;
 constexpr float kBorder = 4.76837158203125e-7f;      // 2^-21
 
@@ -93,20 +95,206 @@ template <typename T> __device__ __forceinline__ void fetch_weights(const NormPa
 // the exact product, or its nearest double-precision number
 template <typename T> __device__ __forceinline__ double exact_sum(T x, T r, bool has_r) { return has_r ? (double)to_float(x) + (double)to_float(r) : (double)to_float(x); }
 
-// What a row's threads share.
-struct Exchange {
-    float ss[kBlock / 32], most[kBlock / 32];
-    double ss_d[kBlock / 32];
-    unsigned long long most_d;
-    int bad;
+// Where single precision leaves no doubt about anything but codes next to the middle between two: the range in which the sums
+// keep their relative error.
+__device__ __forceinline__ bool in_range(Sums s) { return s.ss >= 1e-30f && s.ss <= 1e37f && s.most >= 1e-30f && s.most <= 1e37f; }
+// 127 / most; the reciprocal is within one unit in the last place
+__device__ __forceinline__ float step_inverse(float most)
+{
+    float d;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(d) : "f"(most));
+    return 127.0f * d;
+}
+__device__ __forceinline__ float row_scale(Sums s, int width, float eps) { return s.most / sqrtf(s.ss / (float)width + eps) / 127.0f; }
+
+constexpr float kRound = 12582912.0f;   // 1.5 2^23: adding it leaves the nearest integer in the low bits, ties to even
+
+// Eight codes from the products, and how far the doubtful one of them is into its neighbourhood: above one half, double
+// precision has to decide.
+__device__ __forceinline__ uint2 codes_of(const Pair (&p)[4], float inv, float &doubt)
+{
+    uint32_t t[8];
+    const float near = inv * kBorder;
+    const Pair inv2 = make_pair(inv, inv), round2 = make_pair(kRound, kRound), minus2 = make_pair(-1.0f, -1.0f);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const Pair v = fma2(p[j], inv2, round2), off = fma2(p[j], inv2, fma2(v, minus2, round2));
+        float p0, p1, d0, d1, v0, v1;
+        split(p[j], p0, p1);
+        split(off, d0, d1);
+        split(v, v0, v1);
+        t[2 * j] = __float_as_uint(v0);
+        t[2 * j + 1] = __float_as_uint(v1);
+        doubt = max3(doubt, fmaf(fabsf(p0), near, fabsf(d0)), fmaf(fabsf(p1), near, fabsf(d1)));
+    }
+    return make_uint2(__byte_perm(__byte_perm(t[0], t[1], 0x0040), __byte_perm(t[2], t[3], 0x0040), 0x5410),
+                      __byte_perm(__byte_perm(t[4], t[5], 0x0040), __byte_perm(t[6], t[7], 0x0040), 0x5410));
+}
+
+// What a thread adds to its row's sums: pairs of squares are summed apart.
+struct Partial {
+    Pair ss;
+    float most;
+    __device__ __forceinline__ Partial() : ss(0), most(0.0f) {}
+    __device__ __forceinline__ void add(Pair h, Pair p)
+    {
+        float a, b;
+        split(p, a, b);
+        ss = fma2(h, h, ss);
+        most = max3_abs_nan(most, a, b);
+    }
+    __device__ __forceinline__ Sums sums() const
+    {
+        float a, b;
+        split(ss, a, b);
+        return Sums{a + b, most};
+    }
 };
 
-// One row, held by `threads` threads of which this is number `t`; a warp (kWarp) or the block.
+// A row's sums in double precision.
+struct Exact { double ss, most; };
+__device__ __forceinline__ void add_exact(Exact &e, bool &bad, double h, double p)
+{
+    p = fabs(p);
+    h = fabs(h);
+    e.ss += h * h;
+    e.most = fmax(e.most, p);
+    bad |= !(p <= DBL_MAX) || !(h <= DBL_MAX);
+}
+__device__ __forceinline__ float exact_scale(const Exact &e, bool bad, int width, float eps)
+{
+    return bad ? NAN : e.most > 0.0 ? (float)(e.most / sqrt(e.ss / (double)width + (double)eps) / 127.0) : 0.0f;
+}
+__device__ __forceinline__ uint32_t exact_code(double p, double most) { return (uint32_t)(int)rint(p * 127.0 / most) & 255u; }
+
+// What a row's threads share.
+template <int kThreads> struct ExchangeFor {
+    alignas(16) float ss[kThreads / 32], most[kThreads / 32];
+    double ss_exact[kThreads / 32], most_exact[kThreads / 32];
+    // by every thread of the block, before its first barrier
+    __device__ __forceinline__ void clear(int t, int threads)
+    {
+        for (int k = t; k < kThreads / 32; k += threads) ss[k] = most[k] = 0.0f;
+    }
+};
+typedef ExchangeFor<kBlock> Exchange;
+
+// The threads that hold one row together: a warp, or a block or part of it with a hardware barrier of its own.
+template <bool kWarp> struct Team {
+    int t, threads, barrier;
+    Exchange *sh;
+    __device__ __forceinline__ void sync() const
+    {
+        if (kWarp) __syncwarp();
+        else asm volatile("barrier.cta.sync.aligned %0, %1;" ::"r"(barrier), "r"(threads) : "memory");
+    }
+    __device__ __forceinline__ bool any(bool v) const
+    {
+        if (kWarp) return __any_sync(0xffffffffu, v) != 0;
+        uint32_t r;
+        asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %3, 0;\n\tbarrier.cta.red.or.pred.aligned q, %1, %2, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+                     : "=r"(r) : "r"(barrier), "r"(threads), "r"((uint32_t)v) : "memory");
+        return r != 0;
+    }
+    // every thread gets the row's sums; a barrier has to come before the next call
+    __device__ __forceinline__ Sums total(Sums s) const
+    {
+#pragma unroll
+        for (int d = 16; d; d >>= 1) s.ss += __shfl_xor_sync(0xffffffffu, s.ss, d);
+        asm("redux.sync.max.NaN.f32 %0, %1, 0xffffffff;" : "=f"(s.most) : "f"(s.most));
+        if (kWarp || threads == 32) return s;
+        if ((t & 31) == 0) { sh->ss[t >> 5] = s.ss; sh->most[t >> 5] = s.most; }
+        sync();
+        // four warps at a time; the entries of warps that there are not stay zero
+        const float4 *ss = reinterpret_cast<const float4 *>(sh->ss), *most = reinterpret_cast<const float4 *>(sh->most);
+        s = Sums{0.0f, 0.0f};
+        for (int k = 0; k < threads; k += 128) {
+            const float4 a = ss[k >> 7], m = most[k >> 7];
+            s.ss += (a.x + a.y) + (a.z + a.w);
+            s.most = max3_abs_nan(max3_abs_nan(s.most, m.x, m.y), m.z, m.w);
+        }
+        return s;
+    }
+    __device__ __forceinline__ Exact total(Exact e) const
+    {
+#pragma unroll
+        for (int d = 16; d; d >>= 1) {
+            e.ss += __shfl_xor_sync(0xffffffffu, e.ss, d);
+            e.most = fmax(e.most, __shfl_xor_sync(0xffffffffu, e.most, d));
+        }
+        if (kWarp) return e;
+        if ((t & 31) == 0) { sh->ss_exact[t >> 5] = e.ss; sh->most_exact[t >> 5] = e.most; }
+        sync();
+        e = Exact{0.0, 0.0};
+        for (int k = 0; k < threads >> 5; ++k) { e.ss += sh->ss_exact[k]; e.most = fmax(e.most, sh->most_exact[k]); }
+        return e;
+    }
+};
+
+// The part of a row that single precision leaves in doubt: `plain` rows' codes next to the middle between two, any other row
+// altogether (its scale too).  `prod`: the products in single precision; element(i, x, r, w) gives element i mod 8 of this
+// thread's chunk i / 8, `held` has a bit for each that exists.  Few elements of a plain row need it, found by their
+// products, so that the row's other threads do not wait long.
+template <int kN, bool kWarp, typename Element>
+__device__ __forceinline__ void settle(const Team<kWarp> &team, Element element, uint32_t held, const Pair (&prod)[kN][4], bool has_r, bool plain, float single_most, int width, float eps,
+                                       uint2 (&code)[kN], float &scale)
+{
+    const float from = single_most * (1.0f - 4.0f * kBorder), inv = step_inverse(single_most);
+    uint32_t large = held, doubtful = held;
+    if (plain) {
+        large = doubtful = 0;
+#pragma unroll
+        for (int c = 0; c < kN; ++c)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                float p[2];
+                split(prod[c][j], p[0], p[1]);
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const uint32_t bit = 1u << (8 * c + 2 * j + h);
+                    // the largest product is among those that single precision puts near it
+                    if (fabsf(p[h]) >= from) large |= bit;
+                    const float v = fmaf(p[h], inv, kRound) - kRound;
+                    if (fmaf(fabsf(p[h]), inv * kBorder, fabsf(fmaf(p[h], inv, -v))) > 0.5f) doubtful |= bit;
+                }
+            }
+        large &= held;
+        doubtful &= held;
+    }
+    Exact e{0.0, 0.0};
+    bool bad = false;
+    while (large) {
+        const int i = __ffs((int)large) - 1;
+        large &= large - 1;
+        float x, r, w;
+        element(i, x, r, w);
+        const double h = has_r ? (double)x + (double)r : (double)x;
+        add_exact(e, bad, h, h * (double)w);
+    }
+    bad = team.any(bad);
+    e = team.total(e);
+    if (!plain) scale = exact_scale(e, bad, width, eps);
+    while (doubtful) {
+        const int i = __ffs((int)doubtful) - 1;
+        doubtful &= doubtful - 1;
+        float x, r, w;
+        element(i, x, r, w);
+        const uint32_t k = !bad && e.most > 0.0 ? exact_code((has_r ? (double)x + (double)r : (double)x) * (double)w, e.most) : 0u, at = 8 * (i & 3);
+#pragma unroll
+        for (int c = 0; c < kN; ++c) {
+            if (i >> 2 == 2 * c) code[c].x = (code[c].x & ~(255u << at)) | k << at;
+            if (i >> 2 == 2 * c + 1) code[c].y = (code[c].y & ~(255u << at)) | k << at;
+        }
+    }
+    team.sync();
+}
+
+// One row, read straight into registers.
 template <typename T, bool kWarp>
-__device__ void norm_row(const NormParams &p, int64_t row, int t, int threads, Exchange *sh)
+__device__ __forceinline__ void norm_row(const NormParams &p, int64_t row, const Team<kWarp> &team)
 {
     const T *x = static_cast<const T *>(p.x) + row * p.ldx, *r = p.r ? static_cast<const T *>(p.r) + row * p.ldr : nullptr;
-    const int step = p.vec ? 1 : threads;
+    const int t = team.t, threads = team.threads, step = p.vec ? 1 : threads;
     Eight<T> xe[kChunks], re[kChunks];
     int base[kChunks];
 #pragma unroll
@@ -119,133 +307,53 @@ __device__ void norm_row(const NormParams &p, int64_t row, int t, int threads, E
         for (int c = 0; c < kChunks; ++c)
             if (base[c] < p.width) re[c] = fetch(r, base[c], step, p.width, p.vec);
     }
-    Sums s{0.0f, 0.0f};
+    Partial part;
+    Pair prod[kChunks][4];
+    uint32_t held = 0;                  // a bit for each element that exists
 #pragma unroll
     for (int c = 0; c < kChunks; ++c) {
         if (base[c] >= p.width) continue;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) held |= base[c] + j * step < p.width ? 1u << (8 * c + j) : 0u;
         float w[8];
         fetch_weights<T>(p, base[c], step, w);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const float h = r ? to_float(xe[c].v[j]) + to_float(re[c].v[j]) : to_float(xe[c].v[j]);
-            s.ss = fmaf(h, h, s.ss);
-            s.most = max_nan(s.most, fabsf(h * w[j]));
+        for (int j = 0; j < 4; ++j) {
+            const Pair h = r ? add2(pair_of(xe[c], j), pair_of(re[c], j)) : pair_of(xe[c], j);
+            prod[c][j] = mul2(h, make_pair(w[2 * j], w[2 * j + 1]));
+            part.add(h, prod[c][j]);
         }
     }
+    const Sums s = team.total(part.sums());
+    const bool plain = in_range(s);
+    const float inv = step_inverse(s.most);
+    uint2 code[kChunks];
+    float doubt = plain ? 0.0f : 1.0f, scale = t == 0 ? row_scale(s, p.width, p.eps) : 0.0f;
 #pragma unroll
-    for (int d = 16; d; d >>= 1) s = combine(s, Sums{__shfl_xor_sync(0xffffffffu, s.ss, d), __shfl_xor_sync(0xffffffffu, s.most, d)});
-    if (!kWarp) {
-        const int warps = threads >> 5;
-        if ((t & 31) == 0) { sh->ss[t >> 5] = s.ss; sh->most[t >> 5] = s.most; }
-        if (t == 0) { sh->most_d = 0; sh->bad = 0; }
-        __syncthreads();
-        s = Sums{0.0f, 0.0f};
-        for (int k = 0; k < warps; ++k) s = combine(s, Sums{sh->ss[k], sh->most[k]});
-    }
-    if (p.h) {
+    for (int c = 0; c < kChunks; ++c)
+        if (base[c] < p.width) code[c] = codes_of(prod[c], inv, doubt);
+    if (team.any(doubt > 0.5f))
+        settle(team, [&](int i, float &xv, float &rv, float &wv) {
+            const int c = i >> 3, at = (p.vec ? (c * threads + t) * 8 : c * 8 * threads + t) + (i & 7) * step;
+            xv = to_float(x[at]);
+            rv = r ? to_float(r[at]) : 0.0f;
+            wv = weight_at<T>(p, at);
+        }, held, prod, r != nullptr, plain, s.most, p.width, p.eps, code, scale);
+    if (p.h) {                          // last: it may be x or r, from which doubtful codes were computed again
         T *h = static_cast<T *>(p.h) + row * p.ldh;
 #pragma unroll
         for (int c = 0; c < kChunks; ++c) {
             if (base[c] >= p.width) continue;
-            Eight<T> e;
+            Eight<T> e = xe[c];
+            if (r) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) e.v[j] = r ? from_float<T>(to_float(xe[c].v[j]) + to_float(re[c].v[j])) : xe[c].v[j];
+                for (int j = 0; j < 4; ++j) put_pair(e, j, add2(pair_of(xe[c], j), pair_of(re[c], j)));
+            }
             if (p.vec_h && step == 1 && base[c] + 8 <= p.width) store_eight(h + base[c], e);
             else {
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
                     if (base[c] + j * step < p.width) h[base[c] + j * step] = e.v[j];
-            }
-        }
-    }
-    // the range in which single precision keeps the sums' relative error
-    const bool plain = s.ss >= 1e-30f && s.ss <= 1e37f && s.most >= 1e-30f && s.most <= 1e37f;
-    const float inv = 127.0f / s.most;
-    uint2 code[kChunks];
-    unsigned redo[kChunks];             // one bit for each code that double precision decides
-    bool any = !plain;
-#pragma unroll
-    for (int c = 0; c < kChunks; ++c) {
-        code[c] = make_uint2(0, 0);
-        redo[c] = 0;
-        if (base[c] >= p.width) continue;
-        if (!plain) { redo[c] = 0xFFu; continue; }
-        float w[8];
-        fetch_weights<T>(p, base[c], step, w);
-        int k[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const float h = r ? to_float(xe[c].v[j]) + to_float(re[c].v[j]) : to_float(xe[c].v[j]);
-            const float v = h * w[j] * inv, near = rintf(v);
-            k[j] = (int)near;
-            if (0.5f - fabsf(v - near) < fabsf(v) * kBorder) redo[c] |= 1u << j;
-        }
-        any |= redo[c] != 0;
-        code[c].x = (k[0] & 255) | (k[1] & 255) << 8 | (k[2] & 255) << 16 | (unsigned)k[3] << 24;
-        code[c].y = (k[4] & 255) | (k[5] & 255) << 8 | (k[6] & 255) << 16 | (unsigned)k[7] << 24;
-    }
-    any = kWarp ? __any_sync(0xffffffffu, any) : __syncthreads_or(any) != 0;
-    float scale = s.most / sqrtf(s.ss / (float)p.width + p.eps) / 127.0f;
-    if (any) {
-        // the largest product in double precision, among those that single precision puts near it
-        const float from = plain ? s.most * (1.0f - 4.0f * kBorder) : 0.0f;
-        double most = 0.0, ss = 0.0;
-        bool bad = false;
-#pragma unroll
-        for (int c = 0; c < kChunks; ++c) {
-            if (base[c] >= p.width) continue;
-            float w[8];
-            fetch_weights<T>(p, base[c], step, w);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const float h = r ? to_float(xe[c].v[j]) + to_float(re[c].v[j]) : to_float(xe[c].v[j]);
-                if (plain && !(fabsf(h * w[j]) >= from)) continue;
-                const double hd = exact_sum(xe[c].v[j], r ? re[c].v[j] : xe[c].v[j], r != nullptr), pd = fabs(hd * (double)w[j]);
-                if (base[c] + j * step < p.width) {
-                    ss += hd * hd;
-                    bad |= !(pd <= DBL_MAX) || !(fabs(hd) <= DBL_MAX);
-                    most = fmax(most, pd);
-                }
-            }
-        }
-        if (kWarp) {
-#pragma unroll
-            for (int d = 16; d; d >>= 1) {
-                most = fmax(most, __shfl_xor_sync(0xffffffffu, most, d));
-                ss += __shfl_xor_sync(0xffffffffu, ss, d);
-            }
-            bad = __any_sync(0xffffffffu, bad);
-        } else {
-#pragma unroll
-            for (int d = 16; d; d >>= 1) {
-                most = fmax(most, __shfl_xor_sync(0xffffffffu, most, d));
-                ss += __shfl_xor_sync(0xffffffffu, ss, d);
-            }
-            if ((t & 31) == 0) {
-                sh->ss_d[t >> 5] = ss;
-                atomicMax(&sh->most_d, (unsigned long long)__double_as_longlong(most));      // not negative: ordered as an integer
-            }
-            bad = __syncthreads_or(bad) != 0;
-            most = __longlong_as_double((long long)sh->most_d);
-            ss = 0.0;
-            for (int k = 0; k < threads >> 5; ++k) ss += sh->ss_d[k];
-        }
-        if (!plain) scale = bad ? NAN : most > 0.0 ? (float)(most / sqrt(ss / (double)p.width + (double)p.eps) / 127.0) : 0.0f;
-        if (bad || !(most > 0.0)) {
-#pragma unroll
-            for (int c = 0; c < kChunks; ++c) { code[c] = make_uint2(0, 0); redo[c] = 0; }
-        }
-#pragma unroll
-        for (int c = 0; c < kChunks; ++c) {
-            if (!redo[c]) continue;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const int i = base[c] + j * step;
-                if (!(redo[c] >> j & 1) || i >= p.width) continue;
-                const double pd = exact_sum(xe[c].v[j], r ? re[c].v[j] : xe[c].v[j], r != nullptr) * (double)weight_at<T>(p, i);
-                const unsigned k = (unsigned)(int)rint(pd * 127.0 / most) & 255u, at = 8 * (j & 3);
-                unsigned &word = j < 4 ? code[c].x : code[c].y;
-                word = (word & ~(255u << at)) | k << at;
             }
         }
     }
@@ -267,7 +375,9 @@ __device__ void norm_row(const NormParams &p, int64_t row, int t, int threads, E
 template <typename T> __global__ void __launch_bounds__(kBlock) k_norm_block(const __grid_constant__ NormParams p)
 {
     __shared__ Exchange sh;
-    norm_row<T, false>(p, blockIdx.x, threadIdx.x, blockDim.x, &sh);
+    sh.clear(threadIdx.x, blockDim.x);
+    __syncthreads();
+    norm_row<T, false>(p, blockIdx.x, Team<false>{(int)threadIdx.x, (int)blockDim.x, 0, &sh});
 }
 
 // a warp for a row
@@ -275,7 +385,7 @@ constexpr int kWarpRows = 4;
 template <typename T> __global__ void __launch_bounds__(32 * kWarpRows) k_norm_warp(const __grid_constant__ NormParams p)
 {
     const int64_t row = (int64_t)blockIdx.x * kWarpRows + (threadIdx.x >> 5);
-    if (row < p.rows) norm_row<T, true>(p, row, threadIdx.x & 31, 32, nullptr);
+    if (row < p.rows) norm_row<T, true>(p, row, Team<true>{(int)threadIdx.x & 31, 32, 0, nullptr});
 }
 
 // Rows too long for registers: read twice, in double precision throughout (each thread reads again, from the second-level
@@ -333,16 +443,162 @@ template <typename T> __global__ void __launch_bounds__(kBlock) k_norm_long(cons
     }
 }
 
-template <typename T> cudaError_t launch_norm(const NormParams &p, cudaStream_t st)
+// Many rows: persistent blocks whose teams (a row each, one thread for kHeldChunks chunks) bring their next rows into shared memory by
+// bulk copies, kDepth rows ahead, while they work on the present one.  A team keeps its weights in registers from row to row.
+// With a block for a row and loads straight into registers the loads of a row waited for the row before on the same SM.
+constexpr int kRingThreads = 512, kDepth = 3, kMostTeams = 16, kRingSmem = kRingThreads * 128 * kDepth;      // a thread holds 64 bytes of x and of r
+template <typename T> struct RingShape {
+    static constexpr int kHeldChunks = sizeof(T) == 2 ? 4 : 2;
+    static constexpr int kMostWidth = kRingThreads * kHeldChunks * 8;
+};
+template <typename T, typename W> __global__ void __launch_bounds__(kRingThreads, 1) k_norm_ring(const __grid_constant__ NormParams p, int team_threads, int row_bytes)
 {
+    constexpr int kN = RingShape<T>::kHeldChunks;
+    extern __shared__ __align__(128) uint8_t slots[];
+    __shared__ Exchange sh[kMostTeams];
+    __shared__ __align__(8) uint64_t full[kMostTeams][kDepth];
+    __shared__ int failed;
+    const int teams = blockDim.x / team_threads, which = threadIdx.x / team_threads;
+    const Team<false> team{(int)(threadIdx.x % team_threads), team_threads, which, &sh[which]};
+    const int t = team.t;
+    if (threadIdx.x == 0) failed = 0;
+    sh[which].clear(t, team_threads);
+    if (t == 0)
+        for (int d = 0; d < kDepth; ++d) tc::mbar_init(tc::smem_u32(&full[which][d]), 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    __syncthreads();
+    const T *x = static_cast<const T *>(p.x), *r = static_cast<const T *>(p.r);
+    const int slot_bytes = r ? 2 * row_bytes : row_bytes;
+    uint8_t *mine = slots + (size_t)which * kDepth * slot_bytes;
+    const int64_t first = (int64_t)blockIdx.x * teams + which, stride = (int64_t)gridDim.x * teams;
+    const auto fetch_row = [&](int64_t row, int slot) {
+        const uint32_t bar = tc::smem_u32(&full[which][slot]), dst = tc::smem_u32(mine + slot * slot_bytes);
+        tc::mbar_expect_tx(bar, (uint32_t)slot_bytes);
+        tc::bulk_g2s(dst, x + row * p.ldx, (uint32_t)row_bytes, bar);
+        if (r) tc::bulk_g2s(dst + row_bytes, r + row * p.ldr, (uint32_t)row_bytes, bar);
+    };
+    int64_t issued = 0;                 // the team's k-th copy goes to slot k mod kDepth
+    if (t == 0)
+        for (int d = 0; d < kDepth; ++d)
+            if (first + d * stride < p.rows) {
+                fetch_row(first + d * stride, d);
+                ++issued;
+            }
+    Eight<W> w[kN];
+    int base[kN];
+    uint32_t held = 0;
+#pragma unroll
+    for (int c = 0; c < kN; ++c) {
+        base[c] = (c * team_threads + t) * 8;
+        if (base[c] < p.width) held |= 255u << 8 * c;
+        if (base[c] < p.width) w[c] = fetch(static_cast<const W *>(p.w), base[c], 1, p.width, p.vec_w);
+    }
+    int slot = 0, use = 0;
+    for (int64_t row = first; row < p.rows; row += stride) {
+        if (!wait_limited(tc::smem_u32(&full[which][slot]), (uint32_t)use & 1u, &failed)) timeout_word = 1;
+        const T *xs = reinterpret_cast<const T *>(mine + slot * slot_bytes), *rs = reinterpret_cast<const T *>(mine + slot * slot_bytes + row_bytes);
+        Partial part;
+        Pair prod[kN][4];
+#pragma unroll
+        for (int c = 0; c < kN; ++c) {
+            if (base[c] >= p.width) continue;
+            Eight<T> e = *reinterpret_cast<const Eight<T> *>(xs + base[c]), re;
+            if (r) re = *reinterpret_cast<const Eight<T> *>(rs + base[c]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const Pair h = r ? add2(pair_of(e, j), pair_of(re, j)) : pair_of(e, j);
+                prod[c][j] = mul2(h, pair_of(w[c], j));
+                part.add(h, prod[c][j]);
+                if (r) put_pair(e, j, h);
+            }
+            if (p.h) store_eight(static_cast<T *>(p.h) + row * p.ldh + base[c], e);
+        }
+        const Sums s = team.total(part.sums());
+        const bool plain = in_range(s);
+        const float inv = step_inverse(s.most);
+        uint2 code[kN];
+        float doubt = plain ? 0.0f : 1.0f, scale = t == 0 ? row_scale(s, p.width, p.eps) : 0.0f;
+#pragma unroll
+        for (int c = 0; c < kN; ++c)
+            if (base[c] < p.width) code[c] = codes_of(prod[c], inv, doubt);
+        if (team.any(doubt > 0.5f))
+            settle(team, [&](int i, float &xv, float &rv, float &wv) {
+                const int at = ((i >> 3) * team_threads + t) * 8 + (i & 7);
+                xv = to_float(xs[at]);
+                rv = r ? to_float(rs[at]) : 0.0f;
+                wv = weight_at<T>(p, at);
+            }, held, prod, r != nullptr, plain, s.most, p.width, p.eps, code, scale);
+        // all of the team have read the slot
+        if (t == 0) {
+            if (row + kDepth * stride < p.rows && !failed) {
+                fetch_row(row + kDepth * stride, slot);
+                ++issued;
+            }
+            p.scale[row] = failed ? NAN : scale;
+        }
+        int8_t *q = p.q + row * p.ldq;
+#pragma unroll
+        for (int c = 0; c < kN; ++c)
+            if (base[c] < p.width) *reinterpret_cast<uint2 *>(q + base[c]) = code[c];
+        if (++slot == kDepth) { slot = 0; ++use; }
+    }
+    // after a failure copies may still be under way: the block's shared memory stays until they have come, or another limit ends
+    if (t == 0 && failed) {
+        for (int64_t k = issued > kDepth ? issued - kDepth : 0; k < issued; ++k) {
+            int again = 0;
+            wait_limited(tc::smem_u32(&full[which][k % kDepth]), (uint32_t)(k / kDepth) & 1u, &again);
+        }
+    }
+}
+
+// Blocks hold as many teams as fit their threads; the fewer rows, the fewer blocks.  Below two rows for each team of the
+// device nothing would be brought ahead, and a block for a row is as fast.
+template <typename T> cudaError_t launch_ring(const Device &dev, const NormParams &p, cudaStream_t st, bool *taken)
+{
+    constexpr int kPerThread = RingShape<T>::kHeldChunks * 8;
+    *taken = false;
+    const int64_t bytes = (int64_t)p.width * (int64_t)sizeof(T);
+    if (p.width % 8 || !p.vec || !p.vec_h || !p.vec_q || p.width > RingShape<T>::kMostWidth || p.width <= 32 * kPerThread) return cudaSuccess;
+    const int team_threads = ((p.width + kPerThread - 1) / kPerThread + 31) & ~31, teams = std::min(kRingThreads / team_threads, kMostTeams);
+    if (p.rows < 2 * (int64_t)teams * dev.n_sms) return cudaSuccess;
+    const size_t smem = (size_t)teams * kDepth * (size_t)bytes * (p.r ? 2 : 1);
+    void (*const kernel)(NormParams, int, int) = p.wide_w ? k_norm_ring<T, float> : k_norm_ring<T, T>;
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kRingSmem);     // one value: another thread may launch meanwhile
+    if (e != cudaSuccess) return e;
+    *taken = true;
+    kernel<<<(unsigned)dev.n_sms, (unsigned)(teams * team_threads), smem, st>>>(p, team_threads, (int)bytes);
+    return cudaGetLastError();
+}
+
+template <typename T> cudaError_t launch_norm(const Device &dev, const NormParams &p, cudaStream_t st)
+{
+    bool taken;
+    const cudaError_t e = launch_ring<T>(dev, p, st, &taken);
+    if (taken || e != cudaSuccess) return e;
     const int chunks = (p.width + 7) / 8;
     if (p.width > kHeld) k_norm_long<T><<<(unsigned)p.rows, kBlock, 0, st>>>(p);
     else if (chunks <= 32 * kChunks) k_norm_warp<T><<<(unsigned)((p.rows + kWarpRows - 1) / kWarpRows), 32 * kWarpRows, 0, st>>>(p);
-    else k_norm_block<T><<<(unsigned)p.rows, std::max(64, (chunks + kChunks - 1) / kChunks + 31 & ~31), 0, st>>>(p);
+    else k_norm_block<T><<<(unsigned)p.rows, std::max(64, ((chunks + kChunks - 1) / kChunks + 31) & ~31), 0, st>>>(p);
     return cudaGetLastError();
 }
 
 }  // namespace
+
+namespace ops {
+cudaError_t norm_take_timeout(cudaStream_t st, bool *expired)
+{
+    int word = 0;
+    cudaError_t e = cudaMemcpyFromSymbolAsync(&word, timeout_word, sizeof(word), 0, cudaMemcpyDeviceToHost, st);
+    if (e == cudaSuccess) e = cudaStreamSynchronize(st);
+    *expired = word != 0;
+    if (e == cudaSuccess && word) {
+        word = 0;
+        e = cudaMemcpyToSymbolAsync(timeout_word, &word, sizeof(word), 0, cudaMemcpyHostToDevice, st);
+        if (e == cudaSuccess) e = cudaStreamSynchronize(st);
+    }
+    return e;
+}
+}  // namespace ops
 }  // namespace isc
 
 extern "C" int isc_rms_norm_quant(const void *x, int64_t ldx, const void *residual, int64_t ldr, const void *weight, int weight_type, int type, int64_t rows, int64_t width, float eps,
@@ -369,6 +625,8 @@ extern "C" int isc_rms_norm_quant(const void *x, int64_t ldx, const void *residu
     p.vec_h = wide(sum, lds);
     p.vec_q = aligned(q, 8) && (rows == 1 || ldq % 8 == 0);
     const cudaStream_t st = (cudaStream_t)cuda_stream;
-    const cudaError_t e = type == ISC_BF16 ? launch_norm<__nv_bfloat16>(p, st) : type == ISC_F16 ? launch_norm<__half>(p, st) : launch_norm<float>(p, st);
+    Device dev;
+    cudaError_t e = current_device(&dev);
+    if (e == cudaSuccess) e = type == ISC_BF16 ? launch_norm<__nv_bfloat16>(dev, p, st) : type == ISC_F16 ? launch_norm<__half>(dev, p, st) : launch_norm<float>(dev, p, st);
     return status_of(e, "rms_norm_quant");
 }

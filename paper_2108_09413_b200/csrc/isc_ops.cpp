@@ -44,3 +44,12 @@ int status_of(cudaError_t e, const char *what)
 
 }  // namespace ops
 }  // namespace isc
+
+extern "C" int isc_operator_status(void *cuda_stream)
+{
+    using namespace isc::ops;
+    bool norm = false;
+    const cudaError_t e = norm_take_timeout((cudaStream_t)cuda_stream, &norm);
+    if (e != cudaSuccess) return status_of(e, "operator_status");
+    return norm ? ISC_ERR_TIMEOUT : ISC_OK;
+}
