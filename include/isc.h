@@ -406,6 +406,35 @@ int isc_rms_norm_quant(const void *x, int64_t ldx, const void *residual, int64_t
                        float *scale, void *cuda_stream);
 
 /*
+ * isc_quant_linear -- rows of int8 times an int8 matrix, beside the low-rank adapters of the rows' requests:
+ *   y_tn = x_scale_t * (w_scale_n * sum_k x_tk W_nk + scale_a * sum_r B_anr * sum_k A_ark x_tk) + bias_n,   a = ids_t
+ *   x        : [rows][k] int8 (as isc_rms_norm_quant hands on), x_scale : [rows].
+ *   w        : [n][k] int8, w_scale : [n], bias : [n] or NULL.
+ *   adapters : NULL, or a, b : [n_adapters][rank][k] and [n_adapters][n][rank] of `type` (ISC_BF16 or ISC_F16), without
+ *              gaps; scale : [n_adapters]; ids : [rows].  A row whose id is negative has no adapter, one whose id is
+ *              n_adapters or more is NaN.  Rows need no order, but rows of one request side by side share their work.
+ *              Adapters of fewer ranks are filled up with zeros.  What another row's adapter holds (an infinity, say)
+ *              does not reach a row.
+ *   y        : [rows][n] of `y_type` (ISC_BF16, ISC_F16, ISC_F32).
+ *   work     : isc_quant_linear_work_space bytes, 16 bytes aligned, or NULL without adapters; two calls that overlap in
+ *              time (or two graphs that hold one and run at once) need two.
+ * The int8 products are summed exactly; the adapters' inner sums are held in single precision and handed to the second
+ * product as two numbers of `type` (22 bits in ISC_F16, 16 in ISC_BF16).
+ * Requirements, else ISC_ERR_UNSUPPORTED: x, w, a, b 16 bytes aligned, ldx and ldw multiples of 16; k <= 65,536; rank a
+ * multiple of 4 up to 128; rows and n below 2^31 / 2.  Other errors: ISC_ERR_ARG, ISC_ERR_CUDA.
+ */
+typedef struct {
+    const void *a, *b;
+    const float *scale;
+    const int32_t *ids;
+    int32_t type, n_adapters, rank;
+} isc_adapters;
+int isc_quant_linear(const int8_t *x, int64_t ldx, const float *x_scale, int64_t rows, const int8_t *w, int64_t ldw,
+                     const float *w_scale, int64_t k, int64_t n, const float *bias, const isc_adapters *adapters, void *y,
+                     int64_t ldy, int y_type, void *work, int64_t work_bytes, void *cuda_stream);
+int isc_quant_linear_work_space(int64_t rows, int rank, int64_t *out_bytes);
+
+/*
  * isc_log_probs -- per row of logits l, with z_i = scale * (l_i - max l) and S = sum exp(z):
  *   out_log_probs : [rows]  z_target - log S; 0 where the target is negative, NaN where it is `vocab` or more.
  *   out_entropy   : [rows]  log S - sum(exp(z_i) z_i) / S, in nats.

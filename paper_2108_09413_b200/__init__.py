@@ -6,4 +6,4 @@ compiled library (``python -m paper_2108_09413_b200.build``); there is no CPU fa
 """
 from .binding import (IscError, Model, certify_decide, certify_integer_decide, certified_metrics, noise_table, predict_decide, radius_integer, plan_resident, residual_form, residual_product, lib,  # noqa: F401
                       EXPORTS)
-from .operators import log_probs, rms_norm_quant  # noqa: F401
+from .operators import log_probs, quant_linear, rms_norm_quant  # noqa: F401

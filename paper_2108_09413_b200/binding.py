@@ -12,7 +12,7 @@ _LIB_PATH = os.path.join(_HERE, "libisc.so")
 EXPORTS = ["isc_load_qmodel", "isc_free_qmodel", "isc_plan_resident", "isc_predict", "isc_certify", "isc_certify_batch",
            "isc_sample_counts", "isc_sample_counts_static", "isc_decide_certify", "isc_decide_predict", "isc_certify_integer", "isc_decide_certify_integer", "isc_noise_table", "isc_noise_table_rounded", "isc_radius_integer", "isc_certified_metrics",
            "isc_debug_tensor", "isc_debug_wait_timeout", "isc_debug_stalled_launch", "isc_debug_residual_product", "isc_debug_residual_form", "isc_set_option", "isc_get_info", "isc_strerror",
-           "isc_rms_norm_quant", "isc_log_probs", "isc_operator_status"]
+           "isc_rms_norm_quant", "isc_quant_linear", "isc_quant_linear_work_space", "isc_log_probs", "isc_operator_status"]
 
 
 class IscError(RuntimeError):
@@ -76,6 +76,8 @@ def lib():
         i64 = C.c_int64
         L.isc_rms_norm_quant.argtypes = [vp, i64, vp, i64, vp, C.c_int, C.c_int, i64, i64, C.c_float, vp, i64, vp, i64, vp, vp]
         L.isc_log_probs.argtypes = [vp, i64, C.c_int, i64, i64, C.c_float, vp, C.c_int, vp, vp, vp, vp, vp, vp]
+        L.isc_quant_linear.argtypes = [vp, i64, vp, i64, vp, i64, vp, i64, i64, vp, vp, vp, i64, C.c_int, vp, i64, vp]
+        L.isc_quant_linear_work_space.argtypes = [i64, C.c_int, C.POINTER(i64)]
         L.isc_operator_status.argtypes = [vp]
         L.isc_strerror.argtypes = [C.c_int]
         L.isc_strerror.restype = C.c_char_p

@@ -10,7 +10,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libisc.so")
 SOURCES = ["isc_api.cu", "isc_generic.cu", "isc_igemm.cu", "isc_halo.cu", "isc_line.cu", "isc_decide.cpp",
-           "isc_ops.cpp", "isc_norm.cu", "isc_logprobs.cu"]
+           "isc_ops.cpp", "isc_norm.cu", "isc_qlinear.cu", "isc_logprobs.cu"]
 
 
 def _newest_source() -> float:

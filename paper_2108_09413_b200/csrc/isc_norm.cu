@@ -585,19 +585,7 @@ template <typename T> cudaError_t launch_norm(const Device &dev, const NormParam
 }  // namespace
 
 namespace ops {
-cudaError_t norm_take_timeout(cudaStream_t st, bool *expired)
-{
-    int word = 0;
-    cudaError_t e = cudaMemcpyFromSymbolAsync(&word, timeout_word, sizeof(word), 0, cudaMemcpyDeviceToHost, st);
-    if (e == cudaSuccess) e = cudaStreamSynchronize(st);
-    *expired = word != 0;
-    if (e == cudaSuccess && word) {
-        word = 0;
-        e = cudaMemcpyToSymbolAsync(timeout_word, &word, sizeof(word), 0, cudaMemcpyHostToDevice, st);
-        if (e == cudaSuccess) e = cudaStreamSynchronize(st);
-    }
-    return e;
-}
+cudaError_t norm_take_timeout(cudaStream_t st, bool *expired) { return take_timeout(timeout_word, st, expired); }
 }  // namespace ops
 }  // namespace isc
 

@@ -48,8 +48,9 @@ int status_of(cudaError_t e, const char *what)
 extern "C" int isc_operator_status(void *cuda_stream)
 {
     using namespace isc::ops;
-    bool norm = false;
-    const cudaError_t e = norm_take_timeout((cudaStream_t)cuda_stream, &norm);
+    bool norm = false, linear = false;
+    cudaError_t e = norm_take_timeout((cudaStream_t)cuda_stream, &norm);
+    if (e == cudaSuccess) e = linear_take_timeout((cudaStream_t)cuda_stream, &linear);
     if (e != cudaSuccess) return status_of(e, "operator_status");
-    return norm ? ISC_ERR_TIMEOUT : ISC_OK;
+    return norm || linear ? ISC_ERR_TIMEOUT : ISC_OK;
 }

@@ -34,6 +34,21 @@ template <> __device__ __forceinline__ float from_float<float>(float v) { return
 template <> __device__ __forceinline__ __half from_float<__half>(float v) { return __float2half_rn(v); }
 template <> __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
 
+// Reads a kernel file's timeout word after `st`'s work, and clears it.
+template <typename Word> cudaError_t take_timeout(const Word &device_word, cudaStream_t st, bool *expired)
+{
+    int word = 0;
+    cudaError_t e = cudaMemcpyFromSymbolAsync(&word, device_word, sizeof(word), 0, cudaMemcpyDeviceToHost, st);
+    if (e == cudaSuccess) e = cudaStreamSynchronize(st);
+    *expired = word != 0;
+    if (e == cudaSuccess && word) {
+        word = 0;
+        e = cudaMemcpyToSymbolAsync(device_word, &word, sizeof(word), 0, cudaMemcpyHostToDevice, st);
+        if (e == cudaSuccess) e = cudaStreamSynchronize(st);
+    }
+    return e;
+}
+
 // Eight elements as they lie in memory.
 template <typename T> struct alignas(sizeof(T) == 1 ? 8 : 16) Eight { T v[8]; };
 

@@ -1,0 +1,708 @@
+// Rows of int8 times an int8 matrix on the tensor cores, beside the low-rank adapters of many requests (isc_quant_linear).
+//
+//   y_tn = s_t (u_n sum_k x_tk W_nk + c_a sum_r B_anr sum_k A_ark x_tk) + bias_n,   a = id_t
+//
+// Two kernels.  k_adapter_rows computes the inner sums of the rows that have an adapter; k_quant_linear streams W through
+// tcgen05 kind::i8 and adds the outer product in its epilogue, so y is written once.  The second starts while the first runs
+// (programmatic launch) and waits for it only before its first epilogue.
+//
+// k_quant_linear.  The matrix is the MMA's M side (128 outputs), rows are its N side (16 to 256 rows, whatever divides them
+// best), so a call of one row pays for 16 columns of the tensor core and not for 128.  Operands come by tensor copies of 128 bytes of k
+// (128-byte swizzle; outside the matrices zeros).  One warp copies, one issues, eight requantise; accumulators
+// alternate between two ranges of tensor memory, so one tile's epilogue runs under the next one's products.  Where there are
+// fewer tiles than SMs, a cluster of up to eight blocks shares a tile: each takes a part of k, leaves its int32 sums
+// in shared memory and finishes its share of the tile from all of them; integers add up exactly in any order.
+//
+// The outer product in the epilogue: accumulators are read from tensor memory in the same fragments that mma.sync works on, so
+// B's 16 x 16 blocks times 8 rows' inner sums go straight on top of them in registers.  Eight rows at a time, once
+// for each adapter among them; a row takes only its own adapter's result, by selection and not by adding zeros, which would let
+// another adapter's infinities through.
+#include <cuda.h>
+#include <cuda_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include <algorithm>
+#include <cstdio>
+#include <cstdlib>
+
+#include "isc_conv.cuh"
+#include "isc_ops.cuh"
+#include "isc_ops.h"
+
+namespace isc {
+namespace {
+
+using namespace ops;
+using namespace tc;
+
+__device__ int timeout_word;            // not zero: a bounded wait has run out
+
+constexpr int kTileM = 128, kBlockK = 128;
+constexpr int kEpilogueWarps = 8, kThreads = 32 * (2 + kEpilogueWarps);
+constexpr int kMostStages = 12, kMostTileN = 256, kMostSplit = 8;
+constexpr uint32_t kRingBytes = 192 * 1024;
+constexpr uint32_t kStageRow = 80, kStageRowWide = 144;      // bytes from row to row of a warp's output staging (16-bit, 32-bit)
+constexpr uint32_t kStaging = 8 * kStageRowWide;
+constexpr size_t kSmem = kRingBytes + kEpilogueWarps * kStaging + 1024;
+
+struct LinearParams {
+    CUtensorMap map_w, map_x;
+    const float *x_scale, *w_scale, *bias;
+    const void *b;                      // adapters: [adapter][n][rank]
+    const int32_t *ids;
+    const uint4 *inner;                 // [rank / 16][row][4]: four inner sums, their upper and their lower parts
+    const float *factor;                // [rank / 16][row]
+    void *y;
+    int64_t ldy;
+    int rows, n, k_blocks, rank, n_adapters, adapter_type, y_type;
+    int tile_n, tiles_m, tiles_n, split, stages;
+    bool vec_y;
+};
+
+__device__ __forceinline__ void copy_tile(uint32_t dst, const CUtensorMap *map, int x, int y, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+                 ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(bar) : "memory");
+}
+// K-major operand of 128-byte rows, swizzled over 128 bytes, 1024 bytes from one group of eight rows to the next
+__device__ __forceinline__ uint64_t operand(uint32_t addr)
+{
+    return (uint64_t)((addr & 0x3FFFFu) >> 4) | (uint64_t)1 << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
+}
+template <bool kHalf> __device__ __forceinline__ void mma16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
+{
+    if (kHalf)
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+            : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+    else
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+            : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void cluster_sync()
+{
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t in_block(uint32_t addr, int rank)
+{
+    uint32_t a;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(addr), "r"(rank));
+    return a;
+}
+__device__ __forceinline__ int4 read_remote_v4(uint32_t addr)
+{
+    int4 v;
+    asm volatile("ld.shared::cluster.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
+    return v;
+}
+__device__ __forceinline__ int read_remote(uint32_t addr)
+{
+    int v;
+    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
+    return v;
+}
+
+// What a warp's lane needs for its four outputs of a 32-output strip: fragment rows lane / 4 + 8 i.
+struct Strip {
+    int n0;
+    float w_scale[4], bias[4];
+    __device__ __forceinline__ void load(const LinearParams &p, int first, int lane)
+    {
+        n0 = first;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int n = first + (lane >> 2) + 8 * i;
+            w_scale[i] = n < p.n ? __ldg(p.w_scale + n) : 0.0f;
+            bias[i] = p.bias && n < p.n ? __ldg(p.bias + n) : 0.0f;
+        }
+    }
+};
+
+// The adapters' part of 32 outputs x 8 rows, on top of f (outputs lane / 4 + 8 i, rows 2 (lane mod 4) + j).
+template <bool kHalf> __device__ __forceinline__ void add_adapters(const LinearParams &p, const Strip &s, int row0, int lane, float (&f)[4][2])
+{
+    const int g = lane >> 2, c = lane & 3;
+    const int row = row0 + g, id = row < p.rows ? __ldg(p.ids + row) : -1;
+    const int id0 = __shfl_sync(0xffffffffu, id, 8 * c), id1 = __shfl_sync(0xffffffffu, id, 8 * c + 4);
+    const int blocks = (p.rank + 15) >> 4;
+    uint32_t pending = __ballot_sync(0xffffffffu, id >= 0 && id < p.n_adapters);
+    while (pending) {
+        const int a = __shfl_sync(0xffffffffu, id, __ffs((int)pending) - 1);
+        pending &= ~__ballot_sync(0xffffffffu, id == a);
+        const uint16_t *b = static_cast<const uint16_t *>(p.b) + ((int64_t)a * p.n + s.n0 + g) * p.rank + 4 * c;
+        for (int r = 0; r < blocks; ++r) {
+            const bool there = 16 * r + 4 * c < p.rank;
+            uint2 frag[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                frag[i] = there && s.n0 + g + 8 * i < p.n ? __ldg(reinterpret_cast<const uint2 *>(b + (int64_t)8 * i * p.rank + 16 * r)) : make_uint2(0, 0);
+            const uint4 in = id == a ? __ldcg(p.inner + ((int64_t)r * p.rows + row) * 4 + c) : make_uint4(0, 0, 0, 0);
+            const float f0 = id0 == a ? __ldcg(p.factor + (int64_t)r * p.rows + row0 + 2 * c) : 0.0f, f1 = id1 == a ? __ldcg(p.factor + (int64_t)r * p.rows + row0 + 2 * c + 1) : 0.0f;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                float d[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                const uint32_t left[4] = {frag[2 * h].x, frag[2 * h + 1].x, frag[2 * h].y, frag[2 * h + 1].y};
+                mma16<kHalf>(d, left, in.x, in.y);
+                mma16<kHalf>(d, left, in.z, in.w);
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    if (id0 == a) f[2 * h + k][0] = fmaf(f0, d[2 * k], f[2 * h + k][0]);
+                    if (id1 == a) f[2 * h + k][1] = fmaf(f1, d[2 * k + 1], f[2 * h + k][1]);
+                }
+            }
+        }
+    }
+    if (id0 >= p.n_adapters)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f[i][0] = NAN;
+    if (id1 >= p.n_adapters)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f[i][1] = NAN;
+}
+
+// 32 outputs x 8 rows from their sums to y.  acc: fragments of 16 outputs each.  `staging`: this warp's.
+__device__ __forceinline__ void finish(const LinearParams &p, const Strip &s, int row0, int lane, const int (&acc)[2][4], uint32_t staging, bool failed)
+{
+    const int c = lane & 3;
+    float f[4][2];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) f[i][j] = s.w_scale[i] * (float)acc[i >> 1][2 * (i & 1) + j];
+    if (p.rank) {
+        if (p.adapter_type == ISC_F16) add_adapters<true>(p, s, row0, lane, f);
+        else add_adapters<false>(p, s, row0, lane, f);
+    }
+    const float x0 = row0 + 2 * c < p.rows ? __ldg(p.x_scale + row0 + 2 * c) : 0.0f, x1 = row0 + 2 * c + 1 < p.rows ? __ldg(p.x_scale + row0 + 2 * c + 1) : 0.0f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        f[i][0] = failed ? NAN : fmaf(f[i][0], x0, s.bias[i]);
+        f[i][1] = failed ? NAN : fmaf(f[i][1], x1, s.bias[i]);
+    }
+    const int row = row0 + (lane >> 2);
+    __syncwarp();                       // the strip before has been read
+    if (p.y_type != ISC_F32) {
+        uint32_t v[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (p.y_type == ISC_BF16) { const __nv_bfloat162 t = __floats2bfloat162_rn(f[i][0], f[i][1]); v[i] = *reinterpret_cast<const uint32_t *>(&t); }
+            else { const __half2 t = __floats2half2_rn(f[i][0], f[i][1]); v[i] = *reinterpret_cast<const uint32_t *>(&t); }
+        }
+        // four 8 x 8 matrices, transposed: a row of y holds its 32 outputs side by side
+        asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1,%2,%3,%4};"
+                     ::"r"(staging + (uint32_t)(lane & 7) * kStageRow + (uint32_t)(lane >> 3) * 16u), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
+        __syncwarp();
+        const uint4 out = ld_shared_v4(staging + (uint32_t)(lane >> 2) * kStageRow + (uint32_t)c * 16u);
+        if (row < p.rows) {
+            uint16_t *y = static_cast<uint16_t *>(p.y) + (int64_t)row * p.ldy + s.n0 + 8 * c;
+            const int left = p.n - s.n0 - 8 * c;
+            if (p.vec_y && left >= 8) *reinterpret_cast<uint4 *>(y) = out;
+            else {
+                const uint32_t w[4] = {out.x, out.y, out.z, out.w};
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (e < left) y[e] = (uint16_t)(w[e >> 1] >> 16 * (e & 1));
+            }
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+                asm volatile("st.shared.f32 [%0], %1;" ::"r"(staging + (uint32_t)(2 * c + j) * kStageRowWide + (uint32_t)((lane >> 2) + 8 * i) * 4u), "f"(f[i][j]) : "memory");
+        __syncwarp();
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const uint4 out = ld_shared_v4(staging + (uint32_t)(lane >> 2) * kStageRowWide + (uint32_t)(c + 4 * e) * 16u);
+            if (row >= p.rows) continue;
+            uint32_t *y = static_cast<uint32_t *>(p.y) + (int64_t)row * p.ldy + s.n0 + 4 * c + 16 * e;
+            const int left = p.n - s.n0 - 4 * c - 16 * e;
+            if (p.vec_y && left >= 4) *reinterpret_cast<uint4 *>(y) = out;
+            else {
+                const uint32_t w[4] = {out.x, out.y, out.z, out.w};
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    if (q < left) y[q] = w[q];
+            }
+        }
+    }
+}
+
+__global__ void __launch_bounds__(kThreads, 1) k_quant_linear(const __grid_constant__ LinearParams p)
+{
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ __align__(8) uint64_t bar_full[kMostStages], bar_free[kMostStages], bar_acc_full[2], bar_acc_free[2], bar_end;
+    __shared__ uint32_t tmem_addr;
+    __shared__ int failed;
+    const int warp = (int)warp_uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
+    const uint32_t ring = (smem_u32(smem_raw) + 1023u) & ~1023u, staging = ring + kRingBytes;
+    const uint32_t stage_bytes = (uint32_t)(kTileM + p.tile_n) * kBlockK;
+    const int rank = p.split > 1 ? (int)(blockIdx.x % (unsigned)p.split) : 0;
+    const int first_tile = (int)(blockIdx.x / (unsigned)p.split), tile_step = (int)(gridDim.x / (unsigned)p.split), tiles = p.tiles_m * p.tiles_n;
+    const int kb0 = (int)((int64_t)p.k_blocks * rank / p.split), kb1 = (int)((int64_t)p.k_blocks * (rank + 1) / p.split);
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < p.stages; ++s) { mbar_init(smem_u32(&bar_full[s]), 1); mbar_init(smem_u32(&bar_free[s]), 1); }
+        for (int b = 0; b < 2; ++b) { mbar_init(smem_u32(&bar_acc_full[b]), 1); mbar_init(smem_u32(&bar_acc_free[b]), kEpilogueWarps); }
+        mbar_init(smem_u32(&bar_end), 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        failed = 0;
+    }
+    if (warp == 1) tmem_alloc(smem_u32(&tmem_addr), 512);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = tmem_addr;
+
+    if (warp == 0) {
+        if (lane == 0) {
+            int s = 0, use = 0, issued = 0;
+            for (int tile = first_tile; tile < tiles && !failed; tile += tile_step) {
+                const int m0 = tile % p.tiles_m * kTileM, n0 = tile / p.tiles_m * p.tile_n;
+                for (int kb = kb0; kb < kb1; ++kb) {
+                    if (use && !wait_limited(smem_u32(&bar_free[s]), (uint32_t)(use - 1) & 1u, &failed)) { timeout_word = 1; break; }
+                    const uint32_t bar = smem_u32(&bar_full[s]), at = ring + (uint32_t)s * stage_bytes;
+                    mbar_expect_tx(bar, stage_bytes);
+                    copy_tile(at, &p.map_w, kb * kBlockK, m0, bar);
+                    copy_tile(at + kTileM * kBlockK, &p.map_x, kb * kBlockK, n0, bar);
+                    ++issued;
+                    if (++s == p.stages) { s = 0; ++use; }
+                }
+            }
+            // after a failure copies may still be under way
+            if (failed)
+                for (int i = max(0, issued - p.stages); i < issued; ++i) {
+                    int again = 0;
+                    wait_limited(smem_u32(&bar_full[i % p.stages]), (uint32_t)(i / p.stages) & 1u, &again);
+                }
+        }
+        __syncwarp();
+    } else if (warp == 1) {
+        if (lane == 0) {
+            const uint32_t idesc = (2u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(p.tile_n >> 3) << 17) | ((uint32_t)(kTileM >> 4) << 24);
+            int s = 0, use = 0, j = 0;
+            for (int tile = first_tile; tile < tiles && !failed; tile += tile_step, ++j) {
+                const int buf = j & 1;
+                if (j >= 2 && !wait_limited(smem_u32(&bar_acc_free[buf]), (uint32_t)((j >> 1) - 1) & 1u, &failed)) { timeout_word = 1; break; }
+                tc_fence_after();
+                for (int kb = kb0; kb < kb1; ++kb) {
+                    if (!wait_limited(smem_u32(&bar_full[s]), (uint32_t)use & 1u, &failed)) { timeout_word = 1; break; }
+                    tc_fence_after();
+                    const uint64_t a = operand(ring + (uint32_t)s * stage_bytes), b = operand(ring + (uint32_t)s * stage_bytes + kTileM * kBlockK);
+#pragma unroll
+                    for (int q = 0; q < kBlockK / 32; ++q) conv::mma_i8(tmem + (uint32_t)buf * 256u, a + 2 * q, b + 2 * q, idesc, kb > kb0 || q > 0);
+                    conv::commit_to(smem_u32(&bar_free[s]));
+                    if (++s == p.stages) { s = 0; ++use; }
+                }
+                if (!failed) conv::commit_to(smem_u32(&bar_acc_full[buf]));
+            }
+            if (failed) {               // products may still be under way: tensor memory and operands stay until they are done
+                int again = 0;
+                conv::commit_to(smem_u32(&bar_end));
+                wait_limited(smem_u32(&bar_end), 0, &again);
+            }
+        }
+        __syncwarp();
+    } else {
+        const int w = warp - 2, quarter = warp & 3, half = w >> 2;
+        const uint32_t mine = staging + (uint32_t)w * kStaging;
+        Strip strip;
+        if (p.split == 1) {
+            int j = 0;
+            for (int tile = first_tile; tile < tiles; tile += tile_step, ++j) {
+                const int buf = j & 1, n0 = tile / p.tiles_m * p.tile_n;
+                strip.load(p, tile % p.tiles_m * kTileM + 32 * quarter, lane);
+                if (p.rank && j == 0) conv::chain_wait();
+                const bool ok = __all_sync(0xffffffffu, wait_limited(smem_u32(&bar_acc_full[buf]), (uint32_t)(j >> 1) & 1u, &failed)) != 0;
+                if (!ok) timeout_word = 1;
+                tc_fence_after();
+                const uint32_t acc = tmem + (uint32_t)buf * 256u + ((uint32_t)(32 * quarter) << 16);
+                for (int q = half; q < p.tile_n / 16; q += 2) {
+                    int v[2][8];
+                    tmem_ld_frag(acc + 16u * (uint32_t)q, v[0]);
+                    tmem_ld_frag(acc + (16u << 16) + 16u * (uint32_t)q, v[1]);
+                    tmem_ld_frag_wait(v[0]);
+                    tmem_ld_frag_wait(v[1]);
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const int part[2][4] = {{v[0][4 * e], v[0][4 * e + 1], v[0][4 * e + 2], v[0][4 * e + 3]}, {v[1][4 * e], v[1][4 * e + 1], v[1][4 * e + 2], v[1][4 * e + 3]}};
+                        if (n0 + 16 * q + 8 * e < p.rows) finish(p, strip, n0 + 16 * q + 8 * e, lane, part, mine, !ok);
+                    }
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&bar_acc_free[buf]));
+            }
+        } else {
+            // this block's sums to its shared memory; its ring is empty: all products are done
+            const bool ok = __all_sync(0xffffffffu, wait_limited(smem_u32(&bar_acc_full[0]), 0, &failed)) != 0;
+            if (!ok) timeout_word = 1;
+            tc_fence_after();
+            for (int q = half; q < p.tile_n / 16; q += 2) {
+                int v[2][8];
+                tmem_ld_frag(tmem + ((uint32_t)(32 * quarter) << 16) + 16u * (uint32_t)q, v[0]);
+                tmem_ld_frag(tmem + ((uint32_t)(32 * quarter + 16) << 16) + 16u * (uint32_t)q, v[1]);
+                tmem_ld_frag_wait(v[0]);
+                tmem_ld_frag_wait(v[1]);
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const uint32_t item = (uint32_t)(quarter * (p.tile_n / 8) + 2 * q + e);
+                        if (ok) st_shared_v4(ring + ((item * 2 + (uint32_t)h) * 32 + (uint32_t)lane) * 16u,
+                                     make_uint4((uint32_t)v[h][4 * e], (uint32_t)v[h][4 * e + 1], (uint32_t)v[h][4 * e + 2], (uint32_t)v[h][4 * e + 3]));
+                    }
+            }
+            tc_fence_before();
+        }
+    }
+    if (p.split > 1) {
+        __syncwarp();
+        cluster_sync();
+        if (warp >= 2) {
+            const int w = warp - 2, per_quarter = p.tile_n / 8;
+            bool bad = false;
+            for (int b = 0; b < p.split; ++b) bad |= read_remote(in_block(smem_u32(&failed), b)) != 0;
+            if (p.rank) conv::chain_wait();
+            Strip strip;
+            for (int item = rank + p.split * w; item < 4 * per_quarter; item += p.split * kEpilogueWarps) {
+                const int row0 = first_tile / p.tiles_m * p.tile_n + item % per_quarter * 8;
+                if (row0 >= p.rows) continue;
+                int sum[2][4] = {};
+                for (int b = 0; b < p.split; ++b)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const int4 v = read_remote_v4(in_block(ring + (((uint32_t)item * 2 + (uint32_t)h) * 32 + (uint32_t)lane) * 16u, b));
+                        sum[h][0] += v.x; sum[h][1] += v.y; sum[h][2] += v.z; sum[h][3] += v.w;
+                    }
+                strip.load(p, first_tile % p.tiles_m * kTileM + item / per_quarter * 32, lane);
+                finish(p, strip, row0, lane, sum, staging + (uint32_t)w * kStaging, bad);
+            }
+        }
+        __syncwarp();
+        cluster_sync();
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (warp == 1) tmem_dealloc(tmem, 512);
+}
+
+// ---- the adapters' inner sums
+
+struct InnerParams {
+    const int8_t *x;
+    const void *a;                      // [adapter][rank][k]
+    const float *scale;
+    const int32_t *ids;
+    uint4 *inner;
+    float *factor;
+    int64_t ldx;
+    int rows, k, rank, n_adapters, split;
+    bool vec_a;
+};
+
+constexpr int kInnerThreads = 256, kRankBlocks = 2;          // 32 ranks a block
+
+// four int8 as four 16-bit numbers, exactly
+template <bool kHalf> __device__ __forceinline__ uint2 widen(uint32_t v)
+{
+    if (kHalf) {
+        // 1024 + (v + 128), less 1152
+        const uint32_t u = v ^ 0x80808080u, lo = __byte_perm(u, 0x64646464u, 0x4140), hi = __byte_perm(u, 0x64646464u, 0x4342);
+        const __half2 off = __halves2half2(__ushort_as_half(0x6480), __ushort_as_half(0x6480));
+        const __half2 a = __hsub2(*reinterpret_cast<const __half2 *>(&lo), off), b = __hsub2(*reinterpret_cast<const __half2 *>(&hi), off);
+        return make_uint2(*reinterpret_cast<const uint32_t *>(&a), *reinterpret_cast<const uint32_t *>(&b));
+    }
+    // v = (128 + (v & 127)) - (128 or 256), both of them bf16 numbers whose last bits are v's
+    const uint32_t lo = __byte_perm(v, 0x43434343u, 0x4140), hi = __byte_perm(v, 0x43434343u, 0x4342);
+    const uint32_t p0 = lo & 0xFF7FFF7Fu, q0 = lo & 0xFF80FF80u, p1 = hi & 0xFF7FFF7Fu, q1 = hi & 0xFF80FF80u;
+    const __nv_bfloat162 a = __hsub2(*reinterpret_cast<const __nv_bfloat162 *>(&p0), *reinterpret_cast<const __nv_bfloat162 *>(&q0)),
+                         b = __hsub2(*reinterpret_cast<const __nv_bfloat162 *>(&p1), *reinterpret_cast<const __nv_bfloat162 *>(&q1));
+    return make_uint2(*reinterpret_cast<const uint32_t *>(&a), *reinterpret_cast<const uint32_t *>(&b));
+}
+
+// sixteen codes of a row, zeros behind its end (which is read no further: it may be the tensor's)
+__device__ __forceinline__ uint4 load_codes(const int8_t *at, int left)
+{
+    if (left >= 16) return __ldg(reinterpret_cast<const uint4 *>(at));
+    uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+    for (int e = 0; e < 16; ++e)
+        if (e < left) w[e >> 2] |= (uint32_t)(uint8_t)at[e] << 8 * (e & 3);
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// kRowBlocks x 8 rows and 32 ranks for a block (a cluster where k is split): every warp takes one of the rows' adapters and a
+// part of k, ranks on the MMA's M side; the warps' sums meet in shared memory in a fixed order.
+template <bool kHalf, int kRowBlocks> __global__ void __launch_bounds__(kInnerThreads) k_adapter_rows(const __grid_constant__ InnerParams p)
+{
+    constexpr int kRows = 8 * kRowBlocks, kWarps = kInnerThreads / 32, kRanks = 16 * kRankBlocks;
+    __shared__ float4 sums[kWarps][kRankBlocks * kRowBlocks][32];
+    __shared__ float total[kRows][kRanks];
+    __shared__ int ids[kRows], slot_of[kRows], adapter[kRows], n_distinct;
+    conv::chain_start();
+    const int t = threadIdx.x, warp = t >> 5, lane = t & 31, g = lane >> 2, c = lane & 3;
+    const int part = p.split > 1 ? (int)(blockIdx.x % (unsigned)p.split) : 0, row0 = (int)(blockIdx.x / (unsigned)p.split) * kRows, rank0 = blockIdx.y * kRanks;
+    if (warp == 0) {
+        int id = lane < kRows && row0 + lane < p.rows ? p.ids[row0 + lane] : -1;
+        if (id >= p.n_adapters) id = -1;
+        uint32_t pending = __ballot_sync(0xffffffffu, id >= 0);
+        int n = 0, slot = -1;
+        while (pending) {
+            const int a = __shfl_sync(0xffffffffu, id, __ffs((int)pending) - 1);
+            const uint32_t same = __ballot_sync(0xffffffffu, id == a);
+            if (id == a) slot = n;
+            if (lane == 0) adapter[n] = a;
+            pending &= ~same;
+            ++n;
+        }
+        if (lane < kRows) { ids[lane] = id; slot_of[lane] = slot; }
+        if (lane == 0) n_distinct = n;
+    }
+    for (int i = t; i < kRows * kRanks; i += kInnerThreads) total[i / kRanks][i % kRanks] = 0.0f;
+    __syncthreads();
+    const int distinct = n_distinct;
+    const int chunks = (p.k + 63) >> 6, chunk0 = (int)((int64_t)chunks * part / p.split), chunk1 = (int)((int64_t)chunks * (part + 1) / p.split);
+    for (int first = 0; first < distinct; first += kWarps) {
+        const int here = min(distinct - first, kWarps);
+        const int width = here > 4 ? 8 : here > 2 ? 4 : here;        // slots; warps w, w + width, ... share one
+        const int slot = warp % width, share = warp / width, shares = kWarps / width;
+        float acc[kRankBlocks][kRowBlocks][4] = {};
+        if (slot < here) {
+            const int a = adapter[first + slot];
+            const uint16_t *ar[kRankBlocks][2];
+#pragma unroll
+            for (int r = 0; r < kRankBlocks; ++r)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int rank = rank0 + 16 * r + 8 * h + g;
+                    ar[r][h] = rank < p.rank ? static_cast<const uint16_t *>(p.a) + ((int64_t)a * p.rank + rank) * p.k : nullptr;
+                }
+            const int lo = chunk0 + (int)((int64_t)(chunk1 - chunk0) * share / shares), hi = chunk0 + (int)((int64_t)(chunk1 - chunk0) * (share + 1) / shares);
+#pragma unroll 2
+            for (int ch = lo; ch < hi; ++ch) {
+                const int k0 = 64 * ch + 16 * c;
+                uint4 xv[kRowBlocks];
+#pragma unroll
+                for (int b = 0; b < kRowBlocks; ++b) {
+                    const int row = row0 + 8 * b + g;
+                    xv[b] = row < p.rows ? load_codes(p.x + (int64_t)row * p.ldx + k0, p.k - k0) : make_uint4(0, 0, 0, 0);
+                }
+                uint32_t av[kRankBlocks][2][8];
+#pragma unroll
+                for (int r = 0; r < kRankBlocks; ++r)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        if (p.vec_a) {
+#pragma unroll
+                            for (int q = 0; q < 2; ++q) {
+                                const uint4 v = ar[r][h] && k0 + 8 * q < p.k ? __ldg(reinterpret_cast<const uint4 *>(ar[r][h] + k0 + 8 * q)) : make_uint4(0, 0, 0, 0);
+                                av[r][h][4 * q] = v.x; av[r][h][4 * q + 1] = v.y; av[r][h][4 * q + 2] = v.z; av[r][h][4 * q + 3] = v.w;
+                            }
+                        } else {
+#pragma unroll
+                            for (int q = 0; q < 8; ++q) {
+                                const uint32_t e0 = ar[r][h] && k0 + 2 * q < p.k ? ar[r][h][k0 + 2 * q] : 0u, e1 = ar[r][h] && k0 + 2 * q + 1 < p.k ? ar[r][h][k0 + 2 * q + 1] : 0u;
+                                av[r][h][q] = e0 | e1 << 16;
+                            }
+                        }
+                    }
+#pragma unroll
+                for (int s = 0; s < 4; ++s)
+#pragma unroll
+                    for (int b = 0; b < kRowBlocks; ++b) {
+                        const uint2 xb = widen<kHalf>(s == 0 ? xv[b].x : s == 1 ? xv[b].y : s == 2 ? xv[b].z : xv[b].w);
+#pragma unroll
+                        for (int r = 0; r < kRankBlocks; ++r) {
+                            const uint32_t left[4] = {av[r][0][2 * s], av[r][1][2 * s], av[r][0][2 * s + 1], av[r][1][2 * s + 1]};
+                            mma16<kHalf>(acc[r][b], left, xb.x, xb.y);
+                        }
+                    }
+            }
+        }
+#pragma unroll
+        for (int r = 0; r < kRankBlocks; ++r)
+#pragma unroll
+            for (int b = 0; b < kRowBlocks; ++b) sums[warp][r * kRowBlocks + b][lane] = make_float4(acc[r][b][0], acc[r][b][1], acc[r][b][2], acc[r][b][3]);
+        __syncthreads();
+        for (int i = t; i < kRows * kRanks; i += kInnerThreads) {
+            const int row = i / kRanks, rank = i % kRanks, s = slot_of[row] - first;
+            if (s < 0 || s >= here) continue;
+            const int l = (rank & 7) * 4 + ((row & 7) >> 1), e = 2 * ((rank >> 3) & 1) + (row & 1);
+            float v = 0.0f;
+            for (int w = s; w < kWarps; w += width) v += reinterpret_cast<const float *>(&sums[w][(rank >> 4) * kRowBlocks + (row >> 3)][l])[e];
+            total[row][rank] = v;
+        }
+        __syncthreads();
+    }
+    if (p.split > 1) cluster_sync();
+    if (part == 0) {
+        for (int i = t; i < kRows * kRanks; i += kInnerThreads) {
+            const int row = i / kRanks, rank = i % kRanks;
+            float v = total[row][rank];
+            for (int b = 1; b < p.split; ++b) v += __int_as_float(read_remote(in_block(smem_u32(&total[row][rank]), b)));
+            if (rank0 + rank >= p.rank) v = 0.0f;
+            // sixteen ranks share a power of two, so that two numbers of the adapters' type hold a sum without leaving their range
+            float most = fabsf(v);
+#pragma unroll
+            for (int d = 8; d; d >>= 1) most = max_nan(most, __shfl_xor_sync(0xffffffffu, most, d));
+            const uint32_t e = min((__float_as_uint(most) >> 23) + 1u, 253u);
+            const float unit = most > 3.4028234e38f || most != most ? NAN : __uint_as_float(e << 23), part_of = v * __uint_as_float((254u - e) << 23);
+            const int id = ids[row];
+            if (id < 0) continue;
+            const int64_t at = (int64_t)((rank0 + rank) >> 4) * p.rows + row0 + row;
+            if (rank0 + (rank & 16) >= ((p.rank + 15) & ~15)) continue;
+            uint16_t hi, lo;
+            if (kHalf) {
+                const __half h = __float2half_rn(part_of);
+                hi = __half_as_ushort(h);
+                lo = __half_as_ushort(__float2half_rn(part_of - __half2float(h)));
+            } else {
+                const __nv_bfloat16 h = __float2bfloat16_rn(part_of);
+                hi = __bfloat16_as_ushort(h);
+                lo = __bfloat16_as_ushort(__float2bfloat16_rn(part_of - __bfloat162float(h)));
+            }
+            uint16_t *out = reinterpret_cast<uint16_t *>(p.inner + at * 4 + ((rank & 15) >> 2)) + (rank & 3);
+            out[0] = hi;
+            out[4] = lo;
+            if ((rank & 15) == 0) p.factor[at] = unit * p.scale[id];
+        }
+    }
+    if (p.split > 1) cluster_sync();
+}
+
+typedef CUresult (*EncodeFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
+                             CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+bool encode_rows(void *encode, CUtensorMap *map, const int8_t *base, int64_t k, int64_t rows, int64_t ld, int box_rows)
+{
+    const cuuint64_t dims[2] = {(cuuint64_t)k, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)ld};
+    const cuuint32_t box[2] = {kBlockK, (cuuint32_t)box_rows}, step[2] = {1, 1};
+    return ((EncodeFn)encode)(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<int8_t *>(base), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// Row tile, and blocks that share a tile: tiles as even as they can be, and as many blocks at work as there are SMs.
+void plan(LinearParams &p, int n_sms)
+{
+    p.tiles_m = (p.n + kTileM - 1) / kTileM;
+    int64_t best = INT64_MAX;
+    const int least = (p.rows + kMostTileN - 1) / kMostTileN;
+    for (int t = least; t <= std::min(2 * least + 1, least + 32); ++t) {
+        const int width = ((p.rows + t - 1) / t + 15) & ~15, tiles_n = (p.rows + width - 1) / width;
+        const int64_t tiles = (int64_t)p.tiles_m * tiles_n, rounds = (tiles + n_sms - 1) / n_sms;
+        int split = 1;
+        while (split < kMostSplit && tiles * split * 2 <= n_sms && p.k_blocks >= 4 * split) split *= 2;
+        // operands delivered for a block of k, and a fixed share for a tile's start and end
+        const int64_t cost = rounds * ((int64_t)((p.k_blocks + split - 1) / split) * (width + kTileM) + 512 + 2 * width);
+        if (cost < best) {
+            best = cost;
+            p.tile_n = width;
+            p.tiles_n = tiles_n;
+            p.split = split;
+        }
+    }
+    p.stages = std::min<int>(kMostStages, kRingBytes / ((kTileM + p.tile_n) * kBlockK));
+}
+
+template <typename P> cudaError_t launch(void (*kernel)(P), const P &p, dim3 grid, int threads, size_t smem, int cluster, bool chained, cudaStream_t st)
+{
+    cudaLaunchAttribute attr[2];
+    int n = 0;
+    if (cluster > 1) {
+        attr[n].id = cudaLaunchAttributeClusterDimension;
+        attr[n].val.clusterDim.x = (unsigned)cluster;
+        attr[n].val.clusterDim.y = attr[n].val.clusterDim.z = 1;
+        ++n;
+    }
+    if (chained) {
+        attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[n].val.programmaticStreamSerializationAllowed = 1;
+        ++n;
+    }
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cfg.attrs = attr;
+    cfg.numAttrs = (unsigned)n;
+    return cudaLaunchKernelEx(&cfg, kernel, p);
+}
+
+cudaError_t launch_inner(InnerParams p, int type, int n_sms, cudaStream_t st)
+{
+    const int row_blocks = p.rows >= 1024 ? 4 : 1;
+    const int64_t groups = (p.rows + 8 * row_blocks - 1) / (8 * row_blocks), ranks = (p.rank + 16 * kRankBlocks - 1) / (16 * kRankBlocks);
+    p.split = 1;
+    while (p.split < kMostSplit && groups * ranks * p.split * 2 <= 2 * n_sms && p.k >= 64 * 16 * p.split) p.split *= 2;
+    void (*const kernel)(InnerParams) = type == ISC_F16 ? (row_blocks == 4 ? k_adapter_rows<true, 4> : k_adapter_rows<true, 1>) : (row_blocks == 4 ? k_adapter_rows<false, 4> : k_adapter_rows<false, 1>);
+    return launch(kernel, p, dim3((unsigned)(groups * p.split), (unsigned)ranks), kInnerThreads, 0, p.split, false, st);
+}
+
+}  // namespace
+
+namespace ops {
+cudaError_t linear_take_timeout(cudaStream_t st, bool *expired) { return take_timeout(timeout_word, st, expired); }
+}  // namespace ops
+}  // namespace isc
+
+extern "C" int isc_quant_linear_work_space(int64_t rows, int rank, int64_t *out_bytes)
+{
+    if (rows < 0 || rank < 0 || rank > 128 || !out_bytes) return ISC_ERR_ARG;
+    *out_bytes = (int64_t)((rank + 15) / 16) * rows * 68;
+    return ISC_OK;
+}
+
+extern "C" int isc_quant_linear(const int8_t *x, int64_t ldx, const float *x_scale, int64_t rows, const int8_t *w, int64_t ldw, const float *w_scale, int64_t k, int64_t n, const float *bias,
+                                const isc_adapters *adapters, void *y, int64_t ldy, int y_type, void *work, int64_t work_bytes, void *cuda_stream)
+{
+    using namespace isc;
+    using namespace isc::ops;
+    if (rows < 0 || k < 1 || n < 1 || !is_float_type(y_type)) return ISC_ERR_ARG;
+    if (rows == 0) return ISC_OK;
+    if (!x || !x_scale || !w || !w_scale || !y || ldx < k || ldw < k || ldy < n) return ISC_ERR_ARG;
+    if (!aligned(x_scale, 4) || !aligned(w_scale, 4) || !aligned(bias, 4) || !aligned(y, type_bytes(y_type))) return ISC_ERR_ARG;
+    const isc_adapters *ad = adapters;
+    if (ad) {
+        if (!ad->a || !ad->b || !ad->scale || !ad->ids || ad->n_adapters < 1 || ad->rank < 1 || (ad->type != ISC_BF16 && ad->type != ISC_F16)) return ISC_ERR_ARG;
+        if (!aligned(ad->scale, 4) || !aligned(ad->ids, 4) || !work || !aligned(work, 16)) return ISC_ERR_ARG;
+        if (ad->rank % 4 || ad->rank > 128 || !aligned(ad->a, 16) || !aligned(ad->b, 16)) return ISC_ERR_UNSUPPORTED;
+        if (work_bytes < (int64_t)((ad->rank + 15) / 16) * rows * 68) return ISC_ERR_ARG;
+    }
+    // a single row has no pitch
+    if (rows == 1) ldx = (k + 15) & ~(int64_t)15;
+    if (n == 1) ldw = (k + 15) & ~(int64_t)15;
+    // (k: the sums' 32 bits; the rest: 32-bit tile and coordinate arithmetic)
+    if (k > 65536 || rows >= INT32_MAX / 2 || n >= INT32_MAX / 2 || !aligned(x, 16) || !aligned(w, 16) || ldx % 16 || ldw % 16) return ISC_ERR_UNSUPPORTED;
+    Device dev;
+    cudaError_t e = current_device(&dev);
+    if (e != cudaSuccess) return status_of(e, "device");
+    LinearParams p = {};
+    p.x_scale = x_scale; p.w_scale = w_scale; p.bias = bias;
+    p.y = y; p.ldy = ldy; p.y_type = y_type;
+    p.rows = (int)rows; p.n = (int)n; p.k_blocks = (int)((k + kBlockK - 1) / kBlockK);
+    p.vec_y = aligned(y, 16) && ldy * type_bytes(y_type) % 16 == 0;
+    plan(p, dev.n_sms);
+    if ((int64_t)p.tiles_m * p.tiles_n > INT32_MAX / kMostSplit) return ISC_ERR_UNSUPPORTED;
+    if (!dev.encode || !encode_rows(dev.encode, &p.map_w, w, k, n, ldw, kTileM) || !encode_rows(dev.encode, &p.map_x, x, k, rows, ldx, p.tile_n)) return ISC_ERR_CUDA;
+    const cudaStream_t st = (cudaStream_t)cuda_stream;
+    e = cudaFuncSetAttribute(k_quant_linear, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem);
+    if (e != cudaSuccess) return status_of(e, "quant_linear");
+    if (ad) {
+        InnerParams q = {};
+        q.x = x; q.a = ad->a; q.scale = ad->scale; q.ids = ad->ids;
+        q.inner = static_cast<uint4 *>(work);
+        q.factor = reinterpret_cast<float *>(static_cast<uint8_t *>(work) + (int64_t)((ad->rank + 15) / 16) * rows * 64);
+        q.ldx = ldx; q.rows = (int)rows; q.k = (int)k; q.rank = ad->rank; q.n_adapters = ad->n_adapters;
+        q.vec_a = k % 8 == 0;
+        e = launch_inner(q, ad->type, dev.n_sms, st);
+        if (e != cudaSuccess) return status_of(e, "quant_linear, inner sums");
+        p.b = ad->b; p.ids = ad->ids; p.inner = q.inner; p.factor = q.factor;
+        p.rank = ad->rank; p.n_adapters = ad->n_adapters; p.adapter_type = ad->type;
+    }
+    const int tiles = p.tiles_m * p.tiles_n;
+    const unsigned grid = p.split > 1 ? (unsigned)(tiles * p.split) : (unsigned)std::min(tiles, dev.n_sms);
+    e = launch(k_quant_linear, p, dim3(grid), kThreads, kSmem, p.split, ad != nullptr, st);
+    return status_of(e, "quant_linear");
+}

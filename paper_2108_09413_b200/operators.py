@@ -7,6 +7,7 @@ gradients: inputs that require one are refused while gradients are enabled.
 from __future__ import annotations
 
 import contextlib
+import ctypes as C
 
 from .binding import IscError, _check, lib
 
@@ -106,6 +107,64 @@ def rms_norm_quant(x, weight, eps=1e-6, residual=None, sum_out=None, stream=None
         _check(lib().isc_rms_norm_quant(_ptr(x), ldx, _ptr(residual), ldr, _ptr(weight), _type_code(weight), code, rows, width, eps,
                                         _ptr(total), lds, _ptr(q), pitch, _ptr(scale), raw), "isc_rms_norm_quant")
         return (q if pitch == width else q[:, :width]), scale, total
+    return _enqueue(x.device, stream, call)
+
+
+class _Adapters(C.Structure):
+    _fields_ = [("a", C.c_void_p), ("b", C.c_void_p), ("scale", C.c_void_p), ("ids", C.c_void_p), ("type", C.c_int32),
+                ("n_adapters", C.c_int32), ("rank", C.c_int32)]
+
+
+def quant_linear(x, x_scale, w, w_scale, bias=None, adapters=None, adapter_ids=None, out_dtype=None, out=None, stream=None):
+    """[rows, n]: x_scale * (w_scale * (x w^T) + scale B (A x)) + bias, A, B and scale those of each row's adapter.
+    isc_quant_linear.
+
+    x: [rows, k] int8 with x_scale [rows], as rms_norm_quant gives them; w: [n, k] int8 with w_scale [n]; bias: [n] float32.
+    adapters: (A [adapters, rank, k], B [adapters, n, rank], scale [adapters] float32), A and B bfloat16 or float16;
+    adapter_ids: [rows] int32, negative for rows without one.  out_dtype: bfloat16 (the default), float16 or float32;
+    `out`: where the result goes, any row pitch.
+    """
+    import torch
+    what = "quant_linear"
+    a, b, factor = adapters if adapters is not None else (None, None, None)
+    _tensors(what, x, x_scale, w, w_scale, bias, a, b, factor, adapter_ids, out)
+    ldx, ldw = _matrix(what, "x", x, torch.int8), _matrix(what, "w", w, torch.int8)
+    rows, k = x.shape
+    n = w.shape[0]
+    if w.shape[1] != k:
+        _refuse(what, f"w has {w.shape[1]} columns, x {k}")
+    _vector(what, "x_scale", x_scale, torch.float32, rows)
+    _vector(what, "w_scale", w_scale, torch.float32, n)
+    _vector(what, "bias", bias, torch.float32, n)
+    dtype = out.dtype if out is not None else out_dtype if out_dtype is not None else torch.bfloat16
+    if out is not None and out_dtype not in (None, out.dtype):
+        _refuse(what, "out is not of out_dtype")
+    code = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}.get(dtype)
+    if code is None:
+        _refuse(what, "the result is bfloat16, float16 or float32")
+    parts, space = None, 0
+    if adapters is not None:
+        if a.dim() != 3 or b.dim() != 3 or a.dtype not in (torch.bfloat16, torch.float16) or b.dtype != a.dtype:
+            _refuse(what, "adapters are bfloat16 or float16 [adapters, rank, k] and [adapters, n, rank]")
+        count, rank = a.shape[0], a.shape[1]
+        if a.shape[2] != k or tuple(b.shape) != (count, n, rank) or not a.is_contiguous() or not b.is_contiguous():
+            _refuse(what, f"adapters have to be {(count, rank, k)} and {(count, n, rank)} without gaps")
+        _vector(what, "the adapters' scale", factor, torch.float32, count)
+        if adapter_ids is None:
+            _refuse(what, "adapters need adapter_ids")
+        _vector(what, "adapter_ids", adapter_ids, torch.int32, rows)
+        if count:
+            parts = _Adapters(_ptr(a), _ptr(b), _ptr(factor), _ptr(adapter_ids), _type_code(a), count, rank)
+            space = ((rank + 15) // 16) * rows * 68
+
+    def call(raw):
+        y = torch.empty((rows, n), dtype=dtype, device=x.device) if out is None else out
+        ldy = _matrix(what, "out", y, dtype, (rows, n))
+        work = torch.empty(space, dtype=torch.uint8, device=x.device) if space else None
+        _check(lib().isc_quant_linear(_ptr(x), ldx, _ptr(x_scale), rows, _ptr(w), ldw, _ptr(w_scale), k, n, _ptr(bias),
+                                      C.addressof(parts) if parts is not None else None, _ptr(y), ldy, code, _ptr(work), space, raw),
+               "isc_quant_linear")
+        return y
     return _enqueue(x.device, stream, call)
 
 

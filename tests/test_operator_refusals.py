@@ -47,9 +47,56 @@ def test_log_probs(what, value, expected):
     assert changed(isc.lib().isc_log_probs, good, LOGS[what], value) == expected
 
 
+LINEAR = dict(x=0, ldx=1, x_scale=2, rows=3, w=4, ldw=5, w_scale=6, k=7, n=8, bias=9, adapters=10, y=11, ldy=12, y_type=13, work=14, work_bytes=15)
+LINEAR_GOOD = [AT, 64, AT, 8, AT, 64, AT, 64, 100, AT, None, AT, 100, 0, AT, 1 << 20, None]
+
+
+@pytest.mark.parametrize("what,value,expected", [
+    ("x", None, ARG), ("x_scale", None, ARG), ("w", None, ARG), ("w_scale", None, ARG), ("y", None, ARG), ("ldx", 63, ARG), ("ldw", 63, ARG), ("ldy", 99, ARG), ("ldx", 0, ARG),
+    ("x_scale", AT + 2, ARG), ("w_scale", AT + 1, ARG), ("bias", AT + 2, ARG), ("y", AT + 1, ARG), ("y_type", 3, ARG), ("y_type", -1, ARG), ("rows", -1, ARG), ("k", 0, ARG), ("n", 0, ARG),
+    ("x", AT + 8, UNSUPPORTED), ("w", AT + 1, UNSUPPORTED), ("ldx", 72, UNSUPPORTED), ("ldw", 65, UNSUPPORTED), ("rows", 2**30, UNSUPPORTED), ("n", 2**30, UNSUPPORTED), ("k", 65537, UNSUPPORTED),
+    ("rows", 0, OK)])
+def test_linear(what, value, expected):
+    good = list(LINEAR_GOOD)
+    if what == "k" and value > 64:
+        good[LINEAR["ldx"]] = good[LINEAR["ldw"]] = 1 << 20
+    if what == "n" and value > 100:
+        good[LINEAR["ldy"]] = 2**32
+    assert changed(isc.lib().isc_quant_linear, good, LINEAR[what], value) == expected
+
+
+@pytest.mark.parametrize("what,value,expected", [
+    ("a", None, ARG), ("b", None, ARG), ("scale", None, ARG), ("ids", None, ARG), ("scale", AT + 1, ARG), ("ids", AT + 2, ARG), ("type", 2, ARG), ("type", 3, ARG), ("n_adapters", 0, ARG),
+    ("n_adapters", -1, ARG), ("rank", 0, ARG), ("a", AT + 8, UNSUPPORTED), ("b", AT + 2, UNSUPPORTED), ("rank", 6, UNSUPPORTED), ("rank", 132, UNSUPPORTED)])
+def test_linear_s_adapters(what, value, expected):
+    from paper_2108_09413_b200.operators import _Adapters
+    parts = _Adapters(AT, AT, AT, AT, 0, 4, 16)
+    setattr(parts, what, value)
+    good = list(LINEAR_GOOD)
+    good[LINEAR["adapters"]] = C.addressof(parts)
+    assert isc.lib().isc_quant_linear(*good) == expected
+
+
+def test_linear_s_work_space():
+    from paper_2108_09413_b200.operators import _Adapters
+    size = C.c_int64()
+    for rows, rank in ((1, 4), (8, 16), (100, 17), (3, 128)):
+        assert isc.lib().isc_quant_linear_work_space(rows, rank, C.byref(size)) == OK and size.value == -(-rank // 16) * rows * 68
+    for rows, rank in ((-1, 4), (4, -1), (4, 129)):
+        assert isc.lib().isc_quant_linear_work_space(rows, rank, C.byref(size)) == ARG
+    assert isc.lib().isc_quant_linear_work_space(1, 4, None) == ARG
+    parts = _Adapters(AT, AT, AT, AT, 0, 4, 16)
+    for at, value in ((LINEAR["work"], None), (LINEAR["work"], AT + 8), (LINEAR["work_bytes"], 8 * 68 - 1)):
+        good = list(LINEAR_GOOD)
+        good[LINEAR["adapters"]] = C.addressof(parts)
+        good[at] = value
+        assert isc.lib().isc_quant_linear(*good) == ARG
+
+
 def test_tensors_of_the_host_are_refused():
     x, w = torch.zeros(2, 8), torch.ones(8)
-    for call in (lambda: isc.rms_norm_quant(x, w), lambda: isc.log_probs(x), lambda: isc.log_probs([1.0, 2.0])):
+    for call in (lambda: isc.rms_norm_quant(x, w), lambda: isc.log_probs(x), lambda: isc.log_probs([1.0, 2.0]),
+                 lambda: isc.quant_linear(x.to(torch.int8), w, x.to(torch.int8), w)):
         with pytest.raises(isc.IscError) as e:
             call()
         assert e.value.code == ARG
