@@ -418,8 +418,7 @@ int isc_rms_norm_quant(const void *x, int64_t ldx, const void *residual, int64_t
  *   y        : [rows][n] of `y_type` (ISC_BF16, ISC_F16, ISC_F32).
  *   work     : isc_quant_linear_work_space bytes, 16 bytes aligned, or NULL without adapters; two calls that overlap in
  *              time (or two graphs that hold one and run at once) need two.
- * The int8 products are summed exactly; the adapters' inner sums are held in single precision and handed to the second
- * product as two numbers of `type` (22 bits in ISC_F16, 16 in ISC_BF16).
+ * The int8 products are summed exactly; the adapters' sums are held in single precision.
  * Requirements, else ISC_ERR_UNSUPPORTED: x, w, a, b 16 bytes aligned, ldx and ldw multiples of 16; k <= 65,536; rank a
  * multiple of 4 up to 128; rows and n below 2^31 / 2.  Other errors: ISC_ERR_ARG, ISC_ERR_CUDA.
  */

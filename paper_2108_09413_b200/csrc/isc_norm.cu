@@ -185,13 +185,14 @@ template <bool kWarp> struct Team {
     Exchange *sh;
     __device__ __forceinline__ void sync() const
     {
-        if (kWarp) __syncwarp();
-        else asm volatile("barrier.cta.sync.aligned %0, %1;" ::"r"(barrier), "r"(threads) : "memory");
+        __syncwarp();
+        if (!kWarp) asm volatile("barrier.cta.sync.aligned %0, %1;" ::"r"(barrier), "r"(threads) : "memory");
     }
     __device__ __forceinline__ bool any(bool v) const
     {
         if (kWarp) return __any_sync(0xffffffffu, v) != 0;
         uint32_t r;
+        __syncwarp();
         asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %3, 0;\n\tbarrier.cta.red.or.pred.aligned q, %1, %2, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
                      : "=r"(r) : "r"(barrier), "r"(threads), "r"((uint32_t)v) : "memory");
         return r != 0;

@@ -13,10 +13,12 @@
 // fewer tiles than SMs, a cluster of up to eight blocks shares a tile: each takes a part of k, leaves its int32 sums
 // in shared memory and finishes its share of the tile from all of them; integers add up exactly in any order.
 //
-// The outer product in the epilogue: accumulators are read from tensor memory in the same fragments that mma.sync works on, so
-// B's 16 x 16 blocks times 8 rows' inner sums go straight on top of them in registers.  Eight rows at a time, once
-// for each adapter among them; a row takes only its own adapter's result, by selection and not by adding zeros, which would let
-// another adapter's infinities through.
+// The outer product in the epilogue, in single precision by two-number FMAs: accumulators are read from tensor memory as
+// fragments, so a thread has 4 outputs x 4 rows, and an inner sum that it loads serves four products, a value of B another
+// four (with an output to a lane and one row at a time, loads of inner sums took four times as long as the products).  B
+// stays in registers from row to row while rows share an adapter; a row that does not share its neighbours' loads its own.
+// mma.sync for this part is no way out: beside tcgen05 products that keep the tensor pipe busy each one waits for hundreds
+// of cycles (8,192 rows, k = n = 8,192, rank 32: 604 us with it, 400 us for the product without adapters).
 #include <cuda.h>
 #include <cuda_runtime.h>
 #include <math.h>
@@ -44,18 +46,18 @@ constexpr int kMostStages = 12, kMostTileN = 256, kMostSplit = 8;
 constexpr uint32_t kRingBytes = 192 * 1024;
 constexpr uint32_t kStageRow = 80, kStageRowWide = 144;      // bytes from row to row of a warp's output staging (16-bit, 32-bit)
 constexpr uint32_t kStaging = 8 * kStageRowWide;
-constexpr size_t kSmem = kRingBytes + kEpilogueWarps * kStaging + 1024;
+constexpr uint32_t kInnerRow = 80, kInnerStage = 16 * kInnerRow;      // sixteen rows' inner sums of sixteen ranks, rows apart so that four of them are read at once
+constexpr size_t kSmem = kRingBytes + kEpilogueWarps * (kStaging + 2 * kInnerStage) + 1024;
 
 struct LinearParams {
     CUtensorMap map_w, map_x;
     const float *x_scale, *w_scale, *bias;
     const void *b;                      // adapters: [adapter][n][rank]
     const int32_t *ids;
-    const uint4 *inner;                 // [rank / 16][row][4]: four inner sums, their upper and their lower parts
-    const float *factor;                // [rank / 16][row]
+    const float *inner;                 // [row][ranks]: inner sums times the adapter's scale, zeros behind its rank
     void *y;
     int64_t ldy;
-    int rows, n, k_blocks, rank, n_adapters, adapter_type, y_type;
+    int rows, n, k_blocks, rank, ranks, n_adapters, adapter_type, y_type;    // ranks: rank in whole sixteens
     int tile_n, tiles_m, tiles_n, split, stages;
     bool vec_y;
 };
@@ -81,6 +83,7 @@ template <bool kHalf> __device__ __forceinline__ void mma16(float (&d)[4], const
 }
 __device__ __forceinline__ void cluster_sync()
 {
+    __syncwarp();
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 __device__ __forceinline__ uint32_t in_block(uint32_t addr, int rank)
@@ -118,67 +121,106 @@ struct Strip {
     }
 };
 
-// The adapters' part of 32 outputs x 8 rows, on top of f (outputs lane / 4 + 8 i, rows 2 (lane mod 4) + j).
-template <bool kHalf> __device__ __forceinline__ void add_adapters(const LinearParams &p, const Strip &s, int row0, int lane, float (&f)[4][2])
-{
-    const int g = lane >> 2, c = lane & 3;
-    const int row = row0 + g, id = row < p.rows ? __ldg(p.ids + row) : -1;
-    const int id0 = __shfl_sync(0xffffffffu, id, 8 * c), id1 = __shfl_sync(0xffffffffu, id, 8 * c + 4);
-    const int blocks = (p.rank + 15) >> 4;
-    uint32_t pending = __ballot_sync(0xffffffffu, id >= 0 && id < p.n_adapters);
-    while (pending) {
-        const int a = __shfl_sync(0xffffffffu, id, __ffs((int)pending) - 1);
-        pending &= ~__ballot_sync(0xffffffffu, id == a);
-        const uint16_t *b = static_cast<const uint16_t *>(p.b) + ((int64_t)a * p.n + s.n0 + g) * p.rank + 4 * c;
-        for (int r = 0; r < blocks; ++r) {
-            const bool there = 16 * r + 4 * c < p.rank;
-            uint2 frag[4];
+// kE x 8 rows as a lane of an epilogue warp meets them: it has rows row0 + 8 e + 2 (lane mod 4) + j.
+template <int kE> struct Rows {
+    int id[kE][2];
+    float scale[kE][2];
+    template <bool kAdapters> __device__ __forceinline__ void load(const LinearParams &p, int row0, int lane)
+    {
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                frag[i] = there && s.n0 + g + 8 * i < p.n ? __ldg(reinterpret_cast<const uint2 *>(b + (int64_t)8 * i * p.rank + 16 * r)) : make_uint2(0, 0);
-            const uint4 in = id == a ? __ldcg(p.inner + ((int64_t)r * p.rows + row) * 4 + c) : make_uint4(0, 0, 0, 0);
-            const float f0 = id0 == a ? __ldcg(p.factor + (int64_t)r * p.rows + row0 + 2 * c) : 0.0f, f1 = id1 == a ? __ldcg(p.factor + (int64_t)r * p.rows + row0 + 2 * c + 1) : 0.0f;
+        for (int e = 0; e < kE; ++e)
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                float d[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-                const uint32_t left[4] = {frag[2 * h].x, frag[2 * h + 1].x, frag[2 * h].y, frag[2 * h + 1].y};
-                mma16<kHalf>(d, left, in.x, in.y);
-                mma16<kHalf>(d, left, in.z, in.w);
-#pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    if (id0 == a) f[2 * h + k][0] = fmaf(f0, d[2 * k], f[2 * h + k][0]);
-                    if (id1 == a) f[2 * h + k][1] = fmaf(f1, d[2 * k + 1], f[2 * h + k][1]);
-                }
+            for (int j = 0; j < 2; ++j) {
+                const int row = row0 + 8 * e + 2 * (lane & 3) + j;
+                scale[e][j] = row < p.rows ? __ldg(p.x_scale + row) : 0.0f;
+                id[e][j] = kAdapters && row < p.rows ? __ldg(p.ids + row) : -1;
             }
-        }
     }
-    if (id0 >= p.n_adapters)
+};
+
+// Sixteen ranks of B for a lane's four outputs (lane / 4 + 8 i of a strip), as they lie in memory.
+struct Left {
+    uint2 v[4][4];
+    __device__ __forceinline__ void load(const LinearParams &p, int a, int n0, int block, int lane)
+    {
+        const uint16_t *b = static_cast<const uint16_t *>(p.b) + ((int64_t)a * p.n + n0 + (lane >> 2)) * p.rank + 16 * block;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) f[i][0] = NAN;
-    if (id1 >= p.n_adapters)
+        for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) f[i][1] = NAN;
+            for (int q = 0; q < 4; ++q)
+                v[i][q] = 16 * block + 4 * q < p.rank && n0 + (lane >> 2) + 8 * i < p.n ? __ldg(reinterpret_cast<const uint2 *>(b + (int64_t)8 * i * p.rank + 4 * q)) : make_uint2(0, 0);
+    }
+};
+template <bool kHalf> __device__ __forceinline__ Pair widen_pair(uint32_t w)
+{
+    if (kHalf) {
+        const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&w));
+        return make_pair(f.x, f.y);
+    }
+    return make_pair(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u));
 }
 
-// 32 outputs x 8 rows from their sums to y.  acc: fragments of 16 outputs each.  `staging`: this warp's.
-__device__ __forceinline__ void finish(const LinearParams &p, const Strip &s, int row0, int lane, const int (&acc)[2][4], uint32_t staging, bool failed)
+// Sums of products over ranks, even and odd ones apart.
+template <int kE> struct Outer {
+    Pair v[4][kE][2];
+    __device__ __forceinline__ void clear()
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int e = 0; e < kE; ++e) v[i][e][0] = v[i][e][1] = 0;
+    }
+    // sixteen ranks of all rows (kOne < 0) or of row kOne alone; inner(e, j, q): four inner sums of a row
+    template <bool kHalf, int kOne, typename Inner> __device__ __forceinline__ void add(const Left &left, Inner inner)
+    {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            Pair b[4][2];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) { b[i][0] = widen_pair<kHalf>(left.v[i][q].x); b[i][1] = widen_pair<kHalf>(left.v[i][q].y); }
+#pragma unroll
+            for (int e = 0; e < kE; ++e)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    if (kOne >= 0 && kOne != 2 * e + j) continue;
+                    const float4 in = inner(e, j, q);
+                    const Pair lo = make_pair(in.x, in.y), hi = make_pair(in.z, in.w);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) v[i][e][j] = fma2(b[i][1], hi, fma2(b[i][0], lo, v[i][e][j]));
+                }
+        }
+    }
+    __device__ __forceinline__ float sum(int i, int e, int j) const
+    {
+        float a, b;
+        split(v[i][e][j], a, b);
+        return a + b;
+    }
+};
+
+// one row of several in a strip: its own adapter's ranks
+template <bool kHalf, int kE, int kOne, typename Inner> __device__ __forceinline__ void add_own(const LinearParams &p, const Rows<kE> &rows, int n0, int block, int lane, Inner inner, Outer<kE> &outer)
+{
+    const int a = rows.id[kOne >> 1][kOne & 1];
+    if ((unsigned)a >= (unsigned)p.n_adapters) return;
+    Left left;
+    left.load(p, a, n0, block, lane);
+    outer.template add<kHalf, kOne>(left, inner);
+}
+template <bool kHalf, int kE, typename Inner> __device__ __forceinline__ void add_each(const LinearParams &p, const Rows<kE> &rows, int n0, int block, int lane, Inner inner, Outer<kE> &outer)
+{
+    add_own<kHalf, kE, 0>(p, rows, n0, block, lane, inner, outer);
+    add_own<kHalf, kE, 1>(p, rows, n0, block, lane, inner, outer);
+    if constexpr (kE > 1) {
+        add_own<kHalf, kE, 2>(p, rows, n0, block, lane, inner, outer);
+        add_own<kHalf, kE, 3>(p, rows, n0, block, lane, inner, outer);
+    }
+}
+
+// Results of 32 outputs x 8 rows (f: outputs lane / 4 + 8 i, rows row0 + 2 (lane mod 4) + j) to y.  `staging`: this warp's.
+__device__ __forceinline__ void store_rows(const LinearParams &p, const Strip &s, int row0, int lane, const float (&f)[4][2], uint32_t staging)
 {
     const int c = lane & 3;
-    float f[4][2];
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 2; ++j) f[i][j] = s.w_scale[i] * (float)acc[i >> 1][2 * (i & 1) + j];
-    if (p.rank) {
-        if (p.adapter_type == ISC_F16) add_adapters<true>(p, s, row0, lane, f);
-        else add_adapters<false>(p, s, row0, lane, f);
-    }
-    const float x0 = row0 + 2 * c < p.rows ? __ldg(p.x_scale + row0 + 2 * c) : 0.0f, x1 = row0 + 2 * c + 1 < p.rows ? __ldg(p.x_scale + row0 + 2 * c + 1) : 0.0f;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        f[i][0] = failed ? NAN : fmaf(f[i][0], x0, s.bias[i]);
-        f[i][1] = failed ? NAN : fmaf(f[i][1], x1, s.bias[i]);
-    }
     const int row = row0 + (lane >> 2);
     __syncwarp();                       // the strip before has been read
     if (p.y_type != ISC_F32) {
@@ -228,13 +270,44 @@ __device__ __forceinline__ void finish(const LinearParams &p, const Strip &s, in
     }
 }
 
-__global__ void __launch_bounds__(kThreads, 1) k_quant_linear(const __grid_constant__ LinearParams p)
+// The sums' scales, the adapters' part and the offset.  acc: fragments of 16 outputs each, e: which eight rows.
+template <bool kAdapters, int kE> __device__ __forceinline__ void finish(const LinearParams &p, const Strip &s, const Rows<kE> &rows, const Outer<kE> &outer, int row0, int e, int lane,
+                                                                        const int (&acc)[2][4], uint32_t staging, bool failed)
+{
+    float f[4][2];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const float sum = (float)acc[i >> 1][2 * (i & 1) + j];
+            const float v = kAdapters ? fmaf(s.w_scale[i], sum, outer.sum(i, e, j)) : s.w_scale[i] * sum;
+            f[i][j] = failed || (kAdapters && rows.id[e][j] >= p.n_adapters) ? NAN : fmaf(v, rows.scale[e][j], s.bias[i]);
+        }
+    store_rows(p, s, row0 + 8 * e, lane, f, staging);
+}
+
+// The adapters' operands of a block's first tile into the second-level cache: what a call of few rows otherwise waits for at its end.
+__device__ __forceinline__ void prefetch_adapters(const LinearParams &p, int n0, int m0, int w, int lane)
+{
+    const int bytes = min(kTileM, p.n - m0) * p.rank * 2;
+    for (int t = w; t < p.tile_n && n0 + t < p.rows; t += kEpilogueWarps) {
+        const int a = __ldg(p.ids + n0 + t);
+        if ((unsigned)a >= (unsigned)p.n_adapters || (t && __ldg(p.ids + n0 + t - 1) == a)) continue;
+        const char *b = static_cast<const char *>(p.b) + ((int64_t)a * p.n + m0) * p.rank * 2;
+        for (int at = 128 * lane; at < bytes; at += 128 * 32) asm volatile("prefetch.global.L2 [%0];" ::"l"(b + at));
+    }
+}
+
+// kHeld: blocks of sixteen ranks of B that stay in registers from rows to rows, 1 or 2 (0: more than that, loaded for every sixteen rows);
+// -1: no adapters.
+template <int kHeld, bool kHalf> __global__ void __launch_bounds__(kThreads, 1) k_quant_linear(const __grid_constant__ LinearParams p)
 {
     extern __shared__ uint8_t smem_raw[];
     __shared__ __align__(8) uint64_t bar_full[kMostStages], bar_free[kMostStages], bar_acc_full[2], bar_acc_free[2], bar_end;
     __shared__ uint32_t tmem_addr;
     __shared__ int failed;
     const int warp = (int)warp_uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
+    constexpr bool kAdapters = kHeld >= 0;
     const uint32_t ring = (smem_u32(smem_raw) + 1023u) & ~1023u, staging = ring + kRingBytes;
     const uint32_t stage_bytes = (uint32_t)(kTileM + p.tile_n) * kBlockK;
     const int rank = p.split > 1 ? (int)(blockIdx.x % (unsigned)p.split) : 0;
@@ -306,28 +379,85 @@ __global__ void __launch_bounds__(kThreads, 1) k_quant_linear(const __grid_const
         const int w = warp - 2, quarter = warp & 3, half = w >> 2;
         const uint32_t mine = staging + (uint32_t)w * kStaging;
         Strip strip;
+        if (kAdapters && first_tile < tiles) prefetch_adapters(p, first_tile / p.tiles_m * p.tile_n, first_tile % p.tiles_m * kTileM, w, lane);
         if (p.split == 1) {
+            const uint32_t inner_at = staging + kEpilogueWarps * kStaging + (uint32_t)w * 2u * kInnerStage;
+            const int blocks = kAdapters ? p.ranks >> 4 : 1;
+            // sixteen rows' inner sums of sixteen ranks, brought ahead of their use (rows behind the last one: the last one's)
+            const auto fetch_inner = [&](int row0, int block, int slot) {
+                const int row = min(row0 + (lane >> 1), p.rows - 1), half_of = lane & 1;
+                const float *from = p.inner + (int64_t)row * p.ranks + 16 * block + 8 * half_of;
+                const uint32_t to = inner_at + (uint32_t)slot * kInnerStage + (uint32_t)(lane >> 1) * kInnerRow + 32u * (uint32_t)half_of;
+                conv::cp_async16(to, from);
+                conv::cp_async16(to + 16, from + 4);
+                asm volatile("cp.async.commit_group;" ::: "memory");
+            };
+            if (kAdapters) conv::chain_wait();
             int j = 0;
             for (int tile = first_tile; tile < tiles; tile += tile_step, ++j) {
                 const int buf = j & 1, n0 = tile / p.tiles_m * p.tile_n;
                 strip.load(p, tile % p.tiles_m * kTileM + 32 * quarter, lane);
-                if (p.rank && j == 0) conv::chain_wait();
+                Rows<2> rows;
+                rows.load<kAdapters>(p, n0 + 16 * half, lane);
+                Left held[kHeld > 0 ? kHeld : 1];
+                int held_a = -1, slot = 0;
+                if (kAdapters) fetch_inner(n0 + 16 * half, 0, 0);
                 const bool ok = __all_sync(0xffffffffu, wait_limited(smem_u32(&bar_acc_full[buf]), (uint32_t)(j >> 1) & 1u, &failed)) != 0;
                 if (!ok) timeout_word = 1;
                 tc_fence_after();
                 const uint32_t acc = tmem + (uint32_t)buf * 256u + ((uint32_t)(32 * quarter) << 16);
                 for (int q = half; q < p.tile_n / 16; q += 2) {
+                    const int row0 = n0 + 16 * q;
                     int v[2][8];
                     tmem_ld_frag(acc + 16u * (uint32_t)q, v[0]);
                     tmem_ld_frag(acc + (16u << 16) + 16u * (uint32_t)q, v[1]);
+                    Rows<2> next;
+                    next.load<kAdapters>(p, row0 + 32, lane);
+                    Outer<2> outer;
+                    if (kAdapters) {
+                        outer.clear();
+                        const int a = rows.id[0][0];
+                        const int a0 = __shfl_sync(0xffffffffu, a, 0);
+                        const bool same = __all_sync(0xffffffffu, (a == a0) & (a == rows.id[0][1]) & (a == rows.id[1][0]) & (a == rows.id[1][1])) != 0;
+                        if (kHeld > 0 && same && a != held_a && (unsigned)a < (unsigned)p.n_adapters) {
+                            held_a = a;
+#pragma unroll
+                            for (int r = 0; r < (kHeld > 0 ? kHeld : 1); ++r) held[r].load(p, a, strip.n0, r, lane);
+                        }
+#pragma unroll
+                        for (int r = 0; r < (kHeld > 0 ? kHeld : 8); ++r) {
+                            if (r >= blocks) break;
+                            // the next sixteen ranks or rows
+                            if (r + 1 < blocks) fetch_inner(row0, r + 1, slot ^ 1);
+                            else fetch_inner(row0 + 32, 0, slot ^ 1);
+                            asm volatile("cp.async.wait_group 1;" ::: "memory");
+                            __syncwarp();
+                            const uint32_t from = inner_at + (uint32_t)slot * kInnerStage + 2u * (uint32_t)(lane & 3) * kInnerRow;
+                            const auto inner = [&](int e, int jj, int quad) {
+                                float4 f;
+                                asm volatile("ld.shared.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(f.x), "=f"(f.y), "=f"(f.z), "=f"(f.w) : "r"(from + (uint32_t)(8 * e + jj) * kInnerRow + 16u * (uint32_t)quad));
+                                return f;
+                            };
+                            if (same) {
+                                if ((unsigned)a < (unsigned)p.n_adapters) {
+                                    if (kHeld == 0) held[0].load(p, a, strip.n0, r, lane);
+                                    outer.template add<kHalf, -1>(held[kHeld > 0 ? r : 0], inner);
+                                }
+                            } else add_each<kHalf, 2>(p, rows, strip.n0, r, lane, inner, outer);
+                            __syncwarp();
+                            slot ^= 1;
+                        }
+                    }
                     tmem_ld_frag_wait(v[0]);
                     tmem_ld_frag_wait(v[1]);
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
                         const int part[2][4] = {{v[0][4 * e], v[0][4 * e + 1], v[0][4 * e + 2], v[0][4 * e + 3]}, {v[1][4 * e], v[1][4 * e + 1], v[1][4 * e + 2], v[1][4 * e + 3]}};
-                        if (n0 + 16 * q + 8 * e < p.rows) finish(p, strip, n0 + 16 * q + 8 * e, lane, part, mine, !ok);
+                        if (row0 + 8 * e < p.rows) finish<kAdapters, 2>(p, strip, rows, outer, row0, e, lane, part, mine, !ok);
                     }
+                    rows = next;
                 }
+                if (kAdapters) asm volatile("cp.async.wait_all;" ::: "memory");
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(smem_u32(&bar_acc_free[buf]));
@@ -362,11 +492,22 @@ __global__ void __launch_bounds__(kThreads, 1) k_quant_linear(const __grid_const
             const int w = warp - 2, per_quarter = p.tile_n / 8;
             bool bad = false;
             for (int b = 0; b < p.split; ++b) bad |= read_remote(in_block(smem_u32(&failed), b)) != 0;
-            if (p.rank) conv::chain_wait();
+            if (kAdapters) conv::chain_wait();
             Strip strip;
             for (int item = rank + p.split * w; item < 4 * per_quarter; item += p.split * kEpilogueWarps) {
                 const int row0 = first_tile / p.tiles_m * p.tile_n + item % per_quarter * 8;
                 if (row0 >= p.rows) continue;
+                Rows<1> rows;
+                rows.load<kAdapters>(p, row0, lane);
+                strip.load(p, first_tile % p.tiles_m * kTileM + item / per_quarter * 32, lane);
+                Outer<1> outer;
+                if (kAdapters) {
+                    outer.clear();
+                    for (int r = 0; r < p.ranks >> 4; ++r)
+                        add_each<kHalf, 1>(p, rows, strip.n0, r, lane, [&](int, int j, int quad) {
+                            return *reinterpret_cast<const float4 *>(p.inner + (int64_t)(row0 + 2 * (lane & 3) + j) * p.ranks + 16 * r + 4 * quad);
+                        }, outer);
+                }
                 int sum[2][4] = {};
                 for (int b = 0; b < p.split; ++b)
 #pragma unroll
@@ -374,8 +515,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_quant_linear(const __grid_const
                         const int4 v = read_remote_v4(in_block(ring + (((uint32_t)item * 2 + (uint32_t)h) * 32 + (uint32_t)lane) * 16u, b));
                         sum[h][0] += v.x; sum[h][1] += v.y; sum[h][2] += v.z; sum[h][3] += v.w;
                     }
-                strip.load(p, first_tile % p.tiles_m * kTileM + item / per_quarter * 32, lane);
-                finish(p, strip, row0, lane, sum, staging + (uint32_t)w * kStaging, bad);
+                finish<kAdapters, 1>(p, strip, rows, outer, row0, 0, lane, sum, staging + (uint32_t)w * kStaging, bad);
             }
         }
         __syncwarp();
@@ -394,10 +534,9 @@ struct InnerParams {
     const void *a;                      // [adapter][rank][k]
     const float *scale;
     const int32_t *ids;
-    uint4 *inner;
-    float *factor;
+    float *inner;
     int64_t ldx;
-    int rows, k, rank, n_adapters, split;
+    int rows, k, rank, ranks, n_adapters, split;
     bool vec_a;
 };
 
@@ -541,35 +680,15 @@ template <bool kHalf, int kRowBlocks> __global__ void __launch_bounds__(kInnerTh
             const int row = i / kRanks, rank = i % kRanks;
             float v = total[row][rank];
             for (int b = 1; b < p.split; ++b) v += __int_as_float(read_remote(in_block(smem_u32(&total[row][rank]), b)));
-            if (rank0 + rank >= p.rank) v = 0.0f;
-            // sixteen ranks share a power of two, so that two numbers of the adapters' type hold a sum without leaving their range
-            float most = fabsf(v);
-#pragma unroll
-            for (int d = 8; d; d >>= 1) most = max_nan(most, __shfl_xor_sync(0xffffffffu, most, d));
-            const uint32_t e = min((__float_as_uint(most) >> 23) + 1u, 253u);
-            const float unit = most > 3.4028234e38f || most != most ? NAN : __uint_as_float(e << 23), part_of = v * __uint_as_float((254u - e) << 23);
             const int id = ids[row];
-            if (id < 0) continue;
-            const int64_t at = (int64_t)((rank0 + rank) >> 4) * p.rows + row0 + row;
-            if (rank0 + (rank & 16) >= ((p.rank + 15) & ~15)) continue;
-            uint16_t hi, lo;
-            if (kHalf) {
-                const __half h = __float2half_rn(part_of);
-                hi = __half_as_ushort(h);
-                lo = __half_as_ushort(__float2half_rn(part_of - __half2float(h)));
-            } else {
-                const __nv_bfloat16 h = __float2bfloat16_rn(part_of);
-                hi = __bfloat16_as_ushort(h);
-                lo = __bfloat16_as_ushort(__float2bfloat16_rn(part_of - __bfloat162float(h)));
-            }
-            uint16_t *out = reinterpret_cast<uint16_t *>(p.inner + at * 4 + ((rank & 15) >> 2)) + (rank & 3);
-            out[0] = hi;
-            out[4] = lo;
-            if ((rank & 15) == 0) p.factor[at] = unit * p.scale[id];
+            if (id >= 0 && rank0 + rank < p.ranks) p.inner[(int64_t)(row0 + row) * p.ranks + rank0 + rank] = rank0 + rank < p.rank ? v * p.scale[id] : 0.0f;
         }
     }
     if (p.split > 1) cluster_sync();
 }
+
+// a row's inner sums, in single precision and whole sixteens of ranks
+int64_t work_bytes_of(int64_t rows, int rank) { return (int64_t)((rank + 15) & ~15) * rows * 4; }
 
 typedef CUresult (*EncodeFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
                              CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
@@ -650,7 +769,7 @@ cudaError_t linear_take_timeout(cudaStream_t st, bool *expired) { return take_ti
 extern "C" int isc_quant_linear_work_space(int64_t rows, int rank, int64_t *out_bytes)
 {
     if (rows < 0 || rank < 0 || rank > 128 || !out_bytes) return ISC_ERR_ARG;
-    *out_bytes = (int64_t)((rank + 15) / 16) * rows * 68;
+    *out_bytes = isc::work_bytes_of(rows, rank);
     return ISC_OK;
 }
 
@@ -668,7 +787,7 @@ extern "C" int isc_quant_linear(const int8_t *x, int64_t ldx, const float *x_sca
         if (!ad->a || !ad->b || !ad->scale || !ad->ids || ad->n_adapters < 1 || ad->rank < 1 || (ad->type != ISC_BF16 && ad->type != ISC_F16)) return ISC_ERR_ARG;
         if (!aligned(ad->scale, 4) || !aligned(ad->ids, 4) || !work || !aligned(work, 16)) return ISC_ERR_ARG;
         if (ad->rank % 4 || ad->rank > 128 || !aligned(ad->a, 16) || !aligned(ad->b, 16)) return ISC_ERR_UNSUPPORTED;
-        if (work_bytes < (int64_t)((ad->rank + 15) / 16) * rows * 68) return ISC_ERR_ARG;
+        if (work_bytes < isc::work_bytes_of(rows, ad->rank)) return ISC_ERR_ARG;
     }
     // a single row has no pitch
     if (rows == 1) ldx = (k + 15) & ~(int64_t)15;
@@ -687,22 +806,25 @@ extern "C" int isc_quant_linear(const int8_t *x, int64_t ldx, const float *x_sca
     if ((int64_t)p.tiles_m * p.tiles_n > INT32_MAX / kMostSplit) return ISC_ERR_UNSUPPORTED;
     if (!dev.encode || !encode_rows(dev.encode, &p.map_w, w, k, n, ldw, kTileM) || !encode_rows(dev.encode, &p.map_x, x, k, rows, ldx, p.tile_n)) return ISC_ERR_CUDA;
     const cudaStream_t st = (cudaStream_t)cuda_stream;
-    e = cudaFuncSetAttribute(k_quant_linear, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem);
+    const bool half = ad && ad->type == ISC_F16;
+    void (*const kernel)(LinearParams) = !ad ? k_quant_linear<-1, false> : ad->rank <= 16 ? (half ? k_quant_linear<1, true> : k_quant_linear<1, false>) :
+                                         ad->rank <= 32 ? (half ? k_quant_linear<2, true> : k_quant_linear<2, false>) : half ? k_quant_linear<0, true> : k_quant_linear<0, false>;
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem);
     if (e != cudaSuccess) return status_of(e, "quant_linear");
     if (ad) {
         InnerParams q = {};
         q.x = x; q.a = ad->a; q.scale = ad->scale; q.ids = ad->ids;
-        q.inner = static_cast<uint4 *>(work);
-        q.factor = reinterpret_cast<float *>(static_cast<uint8_t *>(work) + (int64_t)((ad->rank + 15) / 16) * rows * 64);
+        q.inner = static_cast<float *>(work);
+        q.ranks = p.ranks = (ad->rank + 15) & ~15;
         q.ldx = ldx; q.rows = (int)rows; q.k = (int)k; q.rank = ad->rank; q.n_adapters = ad->n_adapters;
         q.vec_a = k % 8 == 0;
         e = launch_inner(q, ad->type, dev.n_sms, st);
         if (e != cudaSuccess) return status_of(e, "quant_linear, inner sums");
-        p.b = ad->b; p.ids = ad->ids; p.inner = q.inner; p.factor = q.factor;
+        p.b = ad->b; p.ids = ad->ids; p.inner = q.inner;
         p.rank = ad->rank; p.n_adapters = ad->n_adapters; p.adapter_type = ad->type;
     }
     const int tiles = p.tiles_m * p.tiles_n;
     const unsigned grid = p.split > 1 ? (unsigned)(tiles * p.split) : (unsigned)std::min(tiles, dev.n_sms);
-    e = launch(k_quant_linear, p, dim3(grid), kThreads, kSmem, p.split, ad != nullptr, st);
+    e = launch(kernel, p, dim3(grid), kThreads, kSmem, p.split, ad != nullptr, st);
     return status_of(e, "quant_linear");
 }

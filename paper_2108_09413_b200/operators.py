@@ -155,7 +155,7 @@ def quant_linear(x, x_scale, w, w_scale, bias=None, adapters=None, adapter_ids=N
         _vector(what, "adapter_ids", adapter_ids, torch.int32, rows)
         if count:
             parts = _Adapters(_ptr(a), _ptr(b), _ptr(factor), _ptr(adapter_ids), _type_code(a), count, rank)
-            space = ((rank + 15) // 16) * rows * 68
+            space = ((rank + 15) // 16) * 64 * rows
 
     def call(raw):
         y = torch.empty((rows, n), dtype=dtype, device=x.device) if out is None else out

@@ -81,12 +81,12 @@ def test_linear_s_work_space():
     from paper_2108_09413_b200.operators import _Adapters
     size = C.c_int64()
     for rows, rank in ((1, 4), (8, 16), (100, 17), (3, 128)):
-        assert isc.lib().isc_quant_linear_work_space(rows, rank, C.byref(size)) == OK and size.value == -(-rank // 16) * rows * 68
+        assert isc.lib().isc_quant_linear_work_space(rows, rank, C.byref(size)) == OK and size.value == -(-rank // 16) * rows * 64
     for rows, rank in ((-1, 4), (4, -1), (4, 129)):
         assert isc.lib().isc_quant_linear_work_space(rows, rank, C.byref(size)) == ARG
     assert isc.lib().isc_quant_linear_work_space(1, 4, None) == ARG
     parts = _Adapters(AT, AT, AT, AT, 0, 4, 16)
-    for at, value in ((LINEAR["work"], None), (LINEAR["work"], AT + 8), (LINEAR["work_bytes"], 8 * 68 - 1)):
+    for at, value in ((LINEAR["work"], None), (LINEAR["work"], AT + 8), (LINEAR["work_bytes"], 8 * 64 - 1)):
         good = list(LINEAR_GOOD)
         good[LINEAR["adapters"]] = C.addressof(parts)
         good[at] = value
