@@ -43,14 +43,17 @@ __device__ int timeout_word;            // not zero: a bounded wait has run out
 constexpr int kTileM = 128, kBlockK = 128;
 constexpr int kEpilogueWarps = 8, kThreads = 32 * (2 + kEpilogueWarps);
 constexpr int kMostStages = 12, kMostTileN = 256, kMostSplit = 8;
-constexpr uint32_t kRingBytes = 192 * 1024;
+constexpr uint32_t kRingBytes = 192 * 1024, kRingBytesNarrow = 96 * 1024;
 constexpr uint32_t kStageRow = 80, kStageRowWide = 144;      // bytes from row to row of a warp's output staging (16-bit, 32-bit)
 constexpr uint32_t kStaging = 8 * kStageRowWide;
 constexpr uint32_t kInnerRow = 80, kInnerStage = 16 * kInnerRow;      // sixteen rows' inner sums of sixteen ranks, rows apart so that four of them are read at once
-constexpr size_t kSmem = kRingBytes + kEpilogueWarps * (kStaging + 2 * kInnerStage) + 1024;
+constexpr size_t kSmemPart = kEpilogueWarps * kStaging + 1024, kSmemTiles = kSmemPart + kEpilogueWarps * 2 * kInnerStage;   // beside the stages
+
+enum Form { kTiles, kPart };
 
 struct LinearParams {
     CUtensorMap map_w, map_x;
+    Form form;
     const float *x_scale, *w_scale, *bias;
     const void *b;                      // adapters: [adapter][n][rank]
     const int32_t *ids;
@@ -59,7 +62,18 @@ struct LinearParams {
     int64_t ldy;
     int rows, n, k_blocks, rank, ranks, n_adapters, adapter_type, y_type;    // ranks: rank in whole sixteens
     int tile_n, tiles_m, tiles_n, split, stages;
+    uint32_t ring_bytes, acc_stride;    // shared memory of the stages; tensor-memory columns of an accumulator
     bool vec_y;
+};
+
+struct FewParams {
+    const int8_t *x, *w;
+    const float *x_scale, *w_scale, *bias, *inner;
+    const void *b;
+    const int32_t *ids;
+    void *y;
+    int64_t ldx, ldw, ldy;
+    int rows, n, k, rank, ranks, n_adapters, y_type;
 };
 
 __device__ __forceinline__ void copy_tile(uint32_t dst, const CUtensorMap *map, int x, int y, uint32_t bar)
@@ -132,8 +146,9 @@ template <int kE> struct Rows {
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
                 const int row = row0 + 8 * e + 2 * (lane & 3) + j;
-                scale[e][j] = row < p.rows ? __ldg(p.x_scale + row) : 0.0f;
                 id[e][j] = kAdapters && row < p.rows ? __ldg(p.ids + row) : -1;
+                const float s = row < p.rows ? __ldg(p.x_scale + row) : 0.0f;
+                scale[e][j] = kAdapters && id[e][j] >= p.n_adapters ? NAN : s;
             }
     }
 };
@@ -234,16 +249,16 @@ __device__ __forceinline__ void store_rows(const LinearParams &p, const Strip &s
         asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1,%2,%3,%4};"
                      ::"r"(staging + (uint32_t)(lane & 7) * kStageRow + (uint32_t)(lane >> 3) * 16u), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
         __syncwarp();
-        const uint4 out = ld_shared_v4(staging + (uint32_t)(lane >> 2) * kStageRow + (uint32_t)c * 16u);
-        if (row < p.rows) {
-            uint16_t *y = static_cast<uint16_t *>(p.y) + (int64_t)row * p.ldy + s.n0 + 8 * c;
-            const int left = p.n - s.n0 - 8 * c;
-            if (p.vec_y && left >= 8) *reinterpret_cast<uint4 *>(y) = out;
-            else {
-                const uint32_t w[4] = {out.x, out.y, out.z, out.w};
+        if (p.vec_y && s.n0 + 32 <= p.n) {
+            const uint4 out = ld_shared_v4(staging + (uint32_t)(lane >> 2) * kStageRow + (uint32_t)c * 16u);
+            if (row < p.rows) *reinterpret_cast<uint4 *>(static_cast<uint16_t *>(p.y) + (int64_t)row * p.ldy + s.n0 + 8 * c) = out;
+        } else {
+            // a lane for an output: adjacent bytes all the same
 #pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    if (e < left) y[e] = (uint16_t)(w[e >> 1] >> 16 * (e & 1));
+            for (int r = 0; r < 8; ++r) {
+                uint16_t v;
+                asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(staging + (uint32_t)r * kStageRow + (uint32_t)lane * 2u));
+                if (row0 + r < p.rows && s.n0 + lane < p.n) static_cast<uint16_t *>(p.y)[(int64_t)(row0 + r) * p.ldy + s.n0 + lane] = v;
             }
         }
     } else {
@@ -253,18 +268,17 @@ __device__ __forceinline__ void store_rows(const LinearParams &p, const Strip &s
             for (int j = 0; j < 2; ++j)
                 asm volatile("st.shared.f32 [%0], %1;" ::"r"(staging + (uint32_t)(2 * c + j) * kStageRowWide + (uint32_t)((lane >> 2) + 8 * i) * 4u), "f"(f[i][j]) : "memory");
         __syncwarp();
+        if (p.vec_y && s.n0 + 32 <= p.n) {
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            const uint4 out = ld_shared_v4(staging + (uint32_t)(lane >> 2) * kStageRowWide + (uint32_t)(c + 4 * e) * 16u);
-            if (row >= p.rows) continue;
-            uint32_t *y = static_cast<uint32_t *>(p.y) + (int64_t)row * p.ldy + s.n0 + 4 * c + 16 * e;
-            const int left = p.n - s.n0 - 4 * c - 16 * e;
-            if (p.vec_y && left >= 4) *reinterpret_cast<uint4 *>(y) = out;
-            else {
-                const uint32_t w[4] = {out.x, out.y, out.z, out.w};
+            for (int e = 0; e < 2; ++e) {
+                const uint4 out = ld_shared_v4(staging + (uint32_t)(lane >> 2) * kStageRowWide + (uint32_t)(c + 4 * e) * 16u);
+                if (row < p.rows) *reinterpret_cast<uint4 *>(static_cast<uint32_t *>(p.y) + (int64_t)row * p.ldy + s.n0 + 4 * c + 16 * e) = out;
+            }
+        } else {
 #pragma unroll
-                for (int q = 0; q < 4; ++q)
-                    if (q < left) y[q] = w[q];
+            for (int r = 0; r < 8; ++r) {
+                const uint32_t v = lds32(staging + (uint32_t)r * kStageRowWide + (uint32_t)lane * 4u);
+                if (row0 + r < p.rows && s.n0 + lane < p.n) static_cast<uint32_t *>(p.y)[(int64_t)(row0 + r) * p.ldy + s.n0 + lane] = v;
             }
         }
     }
@@ -272,7 +286,7 @@ __device__ __forceinline__ void store_rows(const LinearParams &p, const Strip &s
 
 // The sums' scales, the adapters' part and the offset.  acc: fragments of 16 outputs each, e: which eight rows.
 template <bool kAdapters, int kE> __device__ __forceinline__ void finish(const LinearParams &p, const Strip &s, const Rows<kE> &rows, const Outer<kE> &outer, int row0, int e, int lane,
-                                                                        const int (&acc)[2][4], uint32_t staging, bool failed)
+                                                                        const int (&acc)[2][4], uint32_t staging)
 {
     float f[4][2];
 #pragma unroll
@@ -281,9 +295,119 @@ template <bool kAdapters, int kE> __device__ __forceinline__ void finish(const L
         for (int j = 0; j < 2; ++j) {
             const float sum = (float)acc[i >> 1][2 * (i & 1) + j];
             const float v = kAdapters ? fmaf(s.w_scale[i], sum, outer.sum(i, e, j)) : s.w_scale[i] * sum;
-            f[i][j] = failed || (kAdapters && rows.id[e][j] >= p.n_adapters) ? NAN : fmaf(v, rows.scale[e][j], s.bias[i]);
+            f[i][j] = fmaf(v, rows.scale[e][j], s.bias[i]);
         }
     store_rows(p, s, row0 + 8 * e, lane, f, staging);
+}
+
+// One row's outer product with 32 outputs of its adapter: kLanes lanes share an output's ranks, eight each, so that a load covers 512
+// adjacent bytes of B; their sums are joined while they are dealt out, which leaves each lane with one output, output_of(lane).
+template <int kLanes> __device__ __forceinline__ int output_of(int lane) { return (lane & (kLanes - 1)) * (32 / kLanes) + lane / kLanes; }
+template <bool kHalf, int kLanes> __device__ __forceinline__ float outer_of(const LinearParams &p, int a, int row, int n0, int lane)
+{
+    const int rank0 = 8 * (lane & (kLanes - 1)), n = n0 + lane / kLanes;
+    const bool there = rank0 < p.rank, second = rank0 + 4 < p.rank;
+    const uint16_t *b = static_cast<const uint16_t *>(p.b) + ((int64_t)a * p.n + n) * p.rank + rank0;
+    const float4 *in = reinterpret_cast<const float4 *>(p.inner + (int64_t)row * p.ranks + rank0);
+    const float4 zero = make_float4(0.0f, 0.0f, 0.0f, 0.0f), s0 = there ? __ldcg(in) : zero, s1 = there ? __ldcg(in + 1) : zero;
+    const Pair in2[4] = {make_pair(s0.x, s0.y), make_pair(s0.z, s0.w), make_pair(s1.x, s1.y), make_pair(s1.z, s1.w)};
+    float v[kLanes];
+    constexpr int kBatch = kLanes < 8 ? kLanes : 8, kStep = 32 / kLanes;
+#pragma unroll
+    for (int first = 0; first < kLanes; first += kBatch) {
+        uint2 w[kBatch][2];
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) {
+            const bool mine = there && n + (first + i) * kStep < p.n;
+            const uint16_t *from = b + (int64_t)(first + i) * kStep * p.rank;
+            if (p.rank % 8 == 0) {
+                const uint4 q = mine ? __ldg(reinterpret_cast<const uint4 *>(from)) : make_uint4(0, 0, 0, 0);
+                w[i][0] = make_uint2(q.x, q.y);
+                w[i][1] = make_uint2(q.z, q.w);
+            } else {
+                w[i][0] = mine ? __ldg(reinterpret_cast<const uint2 *>(from)) : make_uint2(0, 0);
+                w[i][1] = mine && second ? __ldg(reinterpret_cast<const uint2 *>(from + 4)) : make_uint2(0, 0);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) {
+            const Pair sum = fma2(widen_pair<kHalf>(w[i][1].y), in2[3], fma2(widen_pair<kHalf>(w[i][1].x), in2[2], fma2(widen_pair<kHalf>(w[i][0].y), in2[1], mul2(widen_pair<kHalf>(w[i][0].x), in2[0]))));
+            float x, y;
+            split(sum, x, y);
+            v[first + i] = x + y;
+        }
+    }
+#pragma unroll
+    for (int d = kLanes / 2; d; d >>= 1) {
+        const bool upper = lane & d;
+#pragma unroll
+        for (int i = 0; i < d; ++i) {
+            const float give = upper ? v[i] : v[i + d], keep = upper ? v[i + d] : v[i];
+            v[i] = keep + __shfl_xor_sync(0xffffffffu, give, d);
+        }
+    }
+    return v[0];
+}
+
+// Eight rows' sums of one output from the kSplit blocks that share a tile.
+template <int kSplit> __device__ __forceinline__ void gather(uint32_t at, int (&sum)[8], int first = 0)
+{
+    int4 v[kSplit][2];
+#pragma unroll
+    for (int b = 0; b < kSplit; ++b) {
+        const uint32_t from = in_block(at, first + b);
+        v[b][0] = read_remote_v4(from);
+        v[b][1] = read_remote_v4(from + 16u);
+    }
+#pragma unroll
+    for (int b = 0; b < kSplit; ++b) {
+        sum[0] += v[b][0].x; sum[1] += v[b][0].y; sum[2] += v[b][0].z; sum[3] += v[b][0].w;
+        sum[4] += v[b][1].x; sum[5] += v[b][1].y; sum[6] += v[b][1].z; sum[7] += v[b][1].w;
+    }
+}
+
+// 32 outputs x 8 rows of a tile whose sums lie in the shared memory of the blocks that share it ([output][row], at `sums`).
+template <bool kAdapters, bool kHalf, int kLanes> __device__ __forceinline__ void finish_part(const LinearParams &p, int row0, int n0, uint32_t sums, int lane, bool failed)
+{
+    const int out = output_of<kLanes>(lane), n = n0 + out, mine = row0 + (lane & 7);
+    const float w_scale = n < p.n ? __ldg(p.w_scale + n) : 0.0f, bias = p.bias && n < p.n ? __ldg(p.bias + n) : 0.0f, x_scale = mine < p.rows ? __ldg(p.x_scale + mine) : 0.0f;
+    const int id = kAdapters && mine < p.rows ? __ldg(p.ids + mine) : -1;
+    constexpr int kTogether = kLanes < 8 ? 8 / kLanes : 1;       // rows whose operands are loaded together
+    int sums8[8] = {};
+    const uint32_t from = sums + (uint32_t)out * 32u;
+    if (p.split == 1) gather<1>(from, sums8);
+    else if (p.split == 2) gather<2>(from, sums8);
+    else if (p.split == 4) gather<4>(from, sums8);
+    else { gather<4>(from, sums8); gather<4>(from, sums8, 4); }
+#pragma unroll 1
+    for (int t0 = 0; t0 < 8; t0 += kTogether) {
+        if (row0 + t0 >= p.rows) break;
+        float outer[kTogether];
+        int sum[kTogether], a[kTogether];
+#pragma unroll
+        for (int u = 0; u < kTogether; ++u) {
+            a[u] = __shfl_sync(0xffffffffu, id, t0 + u);
+            sum[u] = sums8[u];
+#pragma unroll
+            for (int t = 1; t < 8; ++t)
+                if (t == t0 + u) sum[u] = sums8[t];          // (registers have no index)
+        }
+#pragma unroll
+        for (int u = 0; u < kTogether; ++u) {
+            outer[u] = 0.0f;
+            if (kAdapters && (unsigned)a[u] < (unsigned)p.n_adapters) outer[u] = outer_of<kHalf, kLanes>(p, a[u], row0 + t0 + u, n0, lane);
+        }
+#pragma unroll
+        for (int u = 0; u < kTogether; ++u) {
+            const float scale = __shfl_sync(0xffffffffu, x_scale, t0 + u);
+            const float f = failed || (kAdapters && a[u] >= p.n_adapters) ? NAN : fmaf(fmaf(w_scale, (float)sum[u], outer[u]), scale, bias);
+            if (row0 + t0 + u >= p.rows || n >= p.n) continue;
+            const int64_t at = (int64_t)(row0 + t0 + u) * p.ldy + n;
+            if (p.y_type == ISC_F32) static_cast<float *>(p.y)[at] = f;
+            else if (p.y_type == ISC_F16) static_cast<__half *>(p.y)[at] = __float2half_rn(f);
+            else static_cast<__nv_bfloat16 *>(p.y)[at] = __float2bfloat16_rn(f);
+        }
+    }
 }
 
 // The adapters' operands of a block's first tile into the second-level cache: what a call of few rows otherwise waits for at its end.
@@ -298,9 +422,11 @@ __device__ __forceinline__ void prefetch_adapters(const LinearParams &p, int n0,
     }
 }
 
-// kHeld: blocks of sixteen ranks of B that stay in registers from rows to rows, 1 or 2 (0: more than that, loaded for every sixteen rows);
-// -1: no adapters.
-template <int kHeld, bool kHalf> __global__ void __launch_bounds__(kThreads, 1) k_quant_linear(const __grid_constant__ LinearParams p)
+// kForm kTiles: persistent blocks with tile after tile.  kPart: a tile, or a part of k of one, for a block, two blocks to an SM if
+// the tile is narrow.
+// kHeld: 1: up to sixteen ranks, of which B stays in registers from rows to rows; 0: more, loaded for every sixteen rows (two blocks
+// in registers, which spill a little then: 246 us against 209 at 8,192 rows, k = n = 4,096, rank 32); -1: no adapters.
+template <Form kForm, int kHeld, bool kHalf> __global__ void __launch_bounds__(kThreads, kForm == kPart ? 2 : 1) k_quant_linear(const __grid_constant__ LinearParams p)
 {
     extern __shared__ uint8_t smem_raw[];
     __shared__ __align__(8) uint64_t bar_full[kMostStages], bar_free[kMostStages], bar_acc_full[2], bar_acc_free[2], bar_end;
@@ -308,7 +434,7 @@ template <int kHeld, bool kHalf> __global__ void __launch_bounds__(kThreads, 1) 
     __shared__ int failed;
     const int warp = (int)warp_uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
     constexpr bool kAdapters = kHeld >= 0;
-    const uint32_t ring = (smem_u32(smem_raw) + 1023u) & ~1023u, staging = ring + kRingBytes;
+    const uint32_t ring = (smem_u32(smem_raw) + 1023u) & ~1023u, staging = ring + p.ring_bytes;
     const uint32_t stage_bytes = (uint32_t)(kTileM + p.tile_n) * kBlockK;
     const int rank = p.split > 1 ? (int)(blockIdx.x % (unsigned)p.split) : 0;
     const int first_tile = (int)(blockIdx.x / (unsigned)p.split), tile_step = (int)(gridDim.x / (unsigned)p.split), tiles = p.tiles_m * p.tiles_n;
@@ -320,7 +446,7 @@ template <int kHeld, bool kHalf> __global__ void __launch_bounds__(kThreads, 1) 
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         failed = 0;
     }
-    if (warp == 1) tmem_alloc(smem_u32(&tmem_addr), 512);
+    if (warp == 1) tmem_alloc(smem_u32(&tmem_addr), 2 * p.acc_stride);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -334,7 +460,7 @@ template <int kHeld, bool kHalf> __global__ void __launch_bounds__(kThreads, 1) 
                 for (int kb = kb0; kb < kb1; ++kb) {
                     if (use && !wait_limited(smem_u32(&bar_free[s]), (uint32_t)(use - 1) & 1u, &failed)) { timeout_word = 1; break; }
                     const uint32_t bar = smem_u32(&bar_full[s]), at = ring + (uint32_t)s * stage_bytes;
-                    mbar_expect_tx(bar, stage_bytes);
+                    mbar_expect_tx(bar, (uint32_t)(kTileM + p.tile_n) * kBlockK);
                     copy_tile(at, &p.map_w, kb * kBlockK, m0, bar);
                     copy_tile(at + kTileM * kBlockK, &p.map_x, kb * kBlockK, n0, bar);
                     ++issued;
@@ -362,7 +488,7 @@ template <int kHeld, bool kHalf> __global__ void __launch_bounds__(kThreads, 1) 
                     tc_fence_after();
                     const uint64_t a = operand(ring + (uint32_t)s * stage_bytes), b = operand(ring + (uint32_t)s * stage_bytes + kTileM * kBlockK);
 #pragma unroll
-                    for (int q = 0; q < kBlockK / 32; ++q) conv::mma_i8(tmem + (uint32_t)buf * 256u, a + 2 * q, b + 2 * q, idesc, kb > kb0 || q > 0);
+                    for (int q = 0; q < kBlockK / 32; ++q) conv::mma_i8(tmem + (uint32_t)buf * p.acc_stride, a + 2 * q, b + 2 * q, idesc, kb > kb0 || q > 0);
                     conv::commit_to(smem_u32(&bar_free[s]));
                     if (++s == p.stages) { s = 0; ++use; }
                 }
@@ -379,8 +505,20 @@ template <int kHeld, bool kHalf> __global__ void __launch_bounds__(kThreads, 1) 
         const int w = warp - 2, quarter = warp & 3, half = w >> 2;
         const uint32_t mine = staging + (uint32_t)w * kStaging;
         Strip strip;
+        if constexpr (kForm == kPart) {
+            // what the end needs: scales, offsets and ids into the second-level cache
+            const int n = first_tile % p.tiles_m * kTileM + 32 * w + lane, row = first_tile / p.tiles_m * p.tile_n + 32 * w + lane;
+            if (w < 4 && n < p.n) {
+                asm volatile("prefetch.global.L2 [%0];" ::"l"(p.w_scale + n));
+                if (p.bias) asm volatile("prefetch.global.L2 [%0];" ::"l"(p.bias + n));
+            }
+            if (32 * w < p.tile_n && row < p.rows) {
+                asm volatile("prefetch.global.L2 [%0];" ::"l"(p.x_scale + row));
+                if (kAdapters) asm volatile("prefetch.global.L2 [%0];" ::"l"(p.ids + row));
+            }
+        }
         if (kAdapters && first_tile < tiles) prefetch_adapters(p, first_tile / p.tiles_m * p.tile_n, first_tile % p.tiles_m * kTileM, w, lane);
-        if (p.split == 1) {
+        if constexpr (kForm == kTiles) {
             const uint32_t inner_at = staging + kEpilogueWarps * kStaging + (uint32_t)w * 2u * kInnerStage;
             const int blocks = kAdapters ? p.ranks >> 4 : 1;
             // sixteen rows' inner sums of sixteen ranks, brought ahead of their use (rows behind the last one: the last one's)
@@ -399,13 +537,17 @@ template <int kHeld, bool kHalf> __global__ void __launch_bounds__(kThreads, 1) 
                 strip.load(p, tile % p.tiles_m * kTileM + 32 * quarter, lane);
                 Rows<2> rows;
                 rows.load<kAdapters>(p, n0 + 16 * half, lane);
-                Left held[kHeld > 0 ? kHeld : 1];
+                Left held;
                 int held_a = -1, slot = 0;
                 if (kAdapters) fetch_inner(n0 + 16 * half, 0, 0);
                 const bool ok = __all_sync(0xffffffffu, wait_limited(smem_u32(&bar_acc_full[buf]), (uint32_t)(j >> 1) & 1u, &failed)) != 0;
-                if (!ok) timeout_word = 1;
+                if (!ok) {              // nothing of the tile can be told
+                    timeout_word = 1;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) strip.w_scale[i] = strip.bias[i] = NAN;
+                }
                 tc_fence_after();
-                const uint32_t acc = tmem + (uint32_t)buf * 256u + ((uint32_t)(32 * quarter) << 16);
+                const uint32_t acc = tmem + (uint32_t)buf * p.acc_stride + ((uint32_t)(32 * quarter) << 16);
                 for (int q = half; q < p.tile_n / 16; q += 2) {
                     const int row0 = n0 + 16 * q;
                     int v[2][8];
@@ -421,31 +563,32 @@ template <int kHeld, bool kHalf> __global__ void __launch_bounds__(kThreads, 1) 
                         const bool same = __all_sync(0xffffffffu, (a == a0) & (a == rows.id[0][1]) & (a == rows.id[1][0]) & (a == rows.id[1][1])) != 0;
                         if (kHeld > 0 && same && a != held_a && (unsigned)a < (unsigned)p.n_adapters) {
                             held_a = a;
-#pragma unroll
-                            for (int r = 0; r < (kHeld > 0 ? kHeld : 1); ++r) held[r].load(p, a, strip.n0, r, lane);
+                            held.load(p, a, strip.n0, 0, lane);
                         }
-#pragma unroll
-                        for (int r = 0; r < (kHeld > 0 ? kHeld : 8); ++r) {
-                            if (r >= blocks) break;
-                            // the next sixteen ranks or rows
+                        // inner sums of block r of this step's rows, once the next sixteen ranks or rows are under way
+                        const auto arrived = [&](int r) {
+                            __syncwarp();               // (the slot to be filled has been read)
                             if (r + 1 < blocks) fetch_inner(row0, r + 1, slot ^ 1);
                             else fetch_inner(row0 + 32, 0, slot ^ 1);
                             asm volatile("cp.async.wait_group 1;" ::: "memory");
                             __syncwarp();
-                            const uint32_t from = inner_at + (uint32_t)slot * kInnerStage + 2u * (uint32_t)(lane & 3) * kInnerRow;
-                            const auto inner = [&](int e, int jj, int quad) {
-                                float4 f;
-                                asm volatile("ld.shared.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(f.x), "=f"(f.y), "=f"(f.z), "=f"(f.w) : "r"(from + (uint32_t)(8 * e + jj) * kInnerRow + 16u * (uint32_t)quad));
-                                return f;
-                            };
-                            if (same) {
-                                if ((unsigned)a < (unsigned)p.n_adapters) {
-                                    if (kHeld == 0) held[0].load(p, a, strip.n0, r, lane);
-                                    outer.template add<kHalf, -1>(held[kHeld > 0 ? r : 0], inner);
-                                }
-                            } else add_each<kHalf, 2>(p, rows, strip.n0, r, lane, inner, outer);
-                            __syncwarp();
+                            const uint8_t *from = smem_raw + (inner_at - smem_u32(smem_raw)) + (uint32_t)slot * kInnerStage + 2u * (uint32_t)(lane & 3) * kInnerRow;
                             slot ^= 1;
+                            return [from](int e, int jj, int quad) { return *reinterpret_cast<const float4 *>(from + (uint32_t)(8 * e + jj) * kInnerRow + 16u * (uint32_t)quad); };
+                        };
+                        if (!same) {
+#pragma unroll 1
+                            for (int r = 0; r < blocks; ++r) add_each<kHalf, 2>(p, rows, strip.n0, r, lane, arrived(r), outer);
+                        } else if (kHeld > 0) {
+                            const auto inner = arrived(0);
+                            if ((unsigned)a < (unsigned)p.n_adapters) outer.template add<kHalf, -1>(held, inner);
+                        } else {
+#pragma unroll 1
+                            for (int r = 0; r < blocks; ++r) {
+                                if ((unsigned)a < (unsigned)p.n_adapters) held.load(p, a, strip.n0, r, lane);
+                                const auto inner = arrived(r);
+                                if ((unsigned)a < (unsigned)p.n_adapters) outer.template add<kHalf, -1>(held, inner);
+                            }
                         }
                     }
                     tmem_ld_frag_wait(v[0]);
@@ -453,7 +596,7 @@ template <int kHeld, bool kHalf> __global__ void __launch_bounds__(kThreads, 1) 
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
                         const int part[2][4] = {{v[0][4 * e], v[0][4 * e + 1], v[0][4 * e + 2], v[0][4 * e + 3]}, {v[1][4 * e], v[1][4 * e + 1], v[1][4 * e + 2], v[1][4 * e + 3]}};
-                        if (row0 + 8 * e < p.rows) finish<kAdapters, 2>(p, strip, rows, outer, row0, e, lane, part, mine, !ok);
+                        if (row0 + 8 * e < p.rows) finish<kAdapters, 2>(p, strip, rows, outer, row0, e, lane, part, mine);
                     }
                     rows = next;
                 }
@@ -468,63 +611,144 @@ template <int kHeld, bool kHalf> __global__ void __launch_bounds__(kThreads, 1) 
             if (!ok) timeout_word = 1;
             tc_fence_after();
             for (int q = half; q < p.tile_n / 16; q += 2) {
-                int v[2][8];
-                tmem_ld_frag(tmem + ((uint32_t)(32 * quarter) << 16) + 16u * (uint32_t)q, v[0]);
-                tmem_ld_frag(tmem + ((uint32_t)(32 * quarter + 16) << 16) + 16u * (uint32_t)q, v[1]);
-                tmem_ld_frag_wait(v[0]);
-                tmem_ld_frag_wait(v[1]);
+                int v[16];
+                tmem_ld16_issue(tmem + ((uint32_t)(32 * quarter) << 16) + 16u * (uint32_t)q, v);
+                asm volatile("tcgen05.wait::ld.sync.aligned;" : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]),
+                             "+r"(v[8]), "+r"(v[9]), "+r"(v[10]), "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]), "+r"(v[15]) :: "memory");
+                // [strip][eight rows][output][row]: a lane that finishes eight rows of an output reads two times 16 bytes
 #pragma unroll
-                for (int e = 0; e < 2; ++e)
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const uint32_t item = (uint32_t)(quarter * (p.tile_n / 8) + 2 * q + e);
-                        if (ok) st_shared_v4(ring + ((item * 2 + (uint32_t)h) * 32 + (uint32_t)lane) * 16u,
-                                     make_uint4((uint32_t)v[h][4 * e], (uint32_t)v[h][4 * e + 1], (uint32_t)v[h][4 * e + 2], (uint32_t)v[h][4 * e + 3]));
-                    }
+                for (int e = 0; e < 4; ++e)
+                    if (ok) st_shared_v4(ring + (uint32_t)((quarter * (p.tile_n / 8) + 2 * q + (e >> 1)) * 32 + lane) * 32u + 16u * (uint32_t)(e & 1),
+                                         make_uint4((uint32_t)v[4 * e], (uint32_t)v[4 * e + 1], (uint32_t)v[4 * e + 2], (uint32_t)v[4 * e + 3]));
             }
             tc_fence_before();
         }
     }
-    if (p.split > 1) {
+    if constexpr (kForm == kPart) {
         __syncwarp();
-        cluster_sync();
+        if (p.split > 1) cluster_sync();
+        else __syncthreads();
         if (warp >= 2) {
             const int w = warp - 2, per_quarter = p.tile_n / 8;
             bool bad = false;
             for (int b = 0; b < p.split; ++b) bad |= read_remote(in_block(smem_u32(&failed), b)) != 0;
             if (kAdapters) conv::chain_wait();
-            Strip strip;
-            for (int item = rank + p.split * w; item < 4 * per_quarter; item += p.split * kEpilogueWarps) {
-                const int row0 = first_tile / p.tiles_m * p.tile_n + item % per_quarter * 8;
-                if (row0 >= p.rows) continue;
-                Rows<1> rows;
-                rows.load<kAdapters>(p, row0, lane);
-                strip.load(p, first_tile % p.tiles_m * kTileM + item / per_quarter * 32, lane);
-                Outer<1> outer;
-                if (kAdapters) {
-                    outer.clear();
-                    for (int r = 0; r < p.ranks >> 4; ++r)
-                        add_each<kHalf, 1>(p, rows, strip.n0, r, lane, [&](int, int j, int quad) {
-                            return *reinterpret_cast<const float4 *>(p.inner + (int64_t)(row0 + 2 * (lane & 3) + j) * p.ranks + 16 * r + 4 * quad);
-                        }, outer);
-                }
-                int sum[2][4] = {};
-                for (int b = 0; b < p.split; ++b)
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const int4 v = read_remote_v4(in_block(ring + (((uint32_t)item * 2 + (uint32_t)h) * 32 + (uint32_t)lane) * 16u, b));
-                        sum[h][0] += v.x; sum[h][1] += v.y; sum[h][2] += v.z; sum[h][3] += v.w;
-                    }
-                finish<kAdapters, 1>(p, strip, rows, outer, row0, 0, lane, sum, staging + (uint32_t)w * kStaging, bad);
+            for (int item = rank + p.split * w; item < kTileM / 32 * per_quarter; item += p.split * kEpilogueWarps) {
+                const int at = item % per_quarter * 8, row0 = first_tile / p.tiles_m * p.tile_n + at, strip = item / per_quarter, n0 = first_tile % p.tiles_m * kTileM + 32 * strip;
+                if (row0 >= p.rows || n0 >= p.n) continue;
+                const uint32_t sums = ring + (uint32_t)item * 1024u;
+                if (!kAdapters || p.rank <= 16) finish_part<kAdapters, kHalf, 2>(p, row0, n0, sums, lane, bad);
+                else if (p.rank <= 32) finish_part<kAdapters, kHalf, 4>(p, row0, n0, sums, lane, bad);
+                else if (p.rank <= 64) finish_part<kAdapters, kHalf, 8>(p, row0, n0, sums, lane, bad);
+                else finish_part<kAdapters, kHalf, 16>(p, row0, n0, sums, lane, bad);
             }
         }
         __syncwarp();
-        cluster_sync();
+        if (p.split > 1) cluster_sync();
     }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    if (warp == 1) tmem_dealloc(tmem, 512);
+    if (warp == 1) tmem_dealloc(tmem, 2 * p.acc_stride);
+}
+
+// sixteen codes of a row, zeros behind its end (which is read no further: it may be the tensor's)
+__device__ __forceinline__ uint4 load_codes(const int8_t *at, int left)
+{
+    if (left >= 16) return __ldg(reinterpret_cast<const uint4 *>(at));
+    uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+    for (int e = 0; e < 16; ++e)
+        if (e < left) w[e >> 2] |= (uint32_t)(uint8_t)at[e] << 8 * (e & 3);
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// ---- few rows: W's rows straight into registers
+
+// kRows rows at most times kOut rows of W a warp, products by dp4a.  A tile of the tensor cores' form costs a fixed time (tensor memory, descriptors,
+// barriers, a cluster's join) that a call of few rows does not get back, and reads W in pieces of 128 bytes; here a warp reads
+// 512 bytes of a row of W at a time.
+constexpr int kFewThreads = 256, kFewRows = 1;
+template <int kRows, int kOut, bool kHalf> __global__ void __launch_bounds__(kFewThreads) k_quant_linear_few(const __grid_constant__ FewParams p)
+{
+    const int lane = threadIdx.x & 31, n0 = (int)((blockIdx.x * (unsigned)(kFewThreads / 32) + (threadIdx.x >> 5)) * kOut);
+    if (n0 >= p.n) return;
+    // the adapters' share of this warp's outputs: the first 32 ranks, a rank to a lane
+    uint32_t b[kRows][kOut];
+    int id[kRows];
+    if (p.rank) {
+#pragma unroll
+        for (int t = 0; t < kRows; ++t) {
+            id[t] = t < p.rows ? __ldg(p.ids + t) : -1;
+#pragma unroll
+            for (int o = 0; o < kOut; ++o)
+                b[t][o] = (unsigned)id[t] < (unsigned)p.n_adapters && lane < p.rank && n0 + o < p.n ? __ldg(static_cast<const uint16_t *>(p.b) + ((int64_t)id[t] * p.n + n0 + o) * p.rank + lane) : 0u;
+        }
+    }
+    // this lane's output's scales, ahead of the products
+    const int my_t = lane / kOut, my_n = n0 + lane % kOut;
+    const bool writes = my_t < p.rows && my_t < kRows && my_n < p.n;
+    const float w_scale = writes ? __ldg(p.w_scale + my_n) : 0.0f, x_scale = writes ? __ldg(p.x_scale + my_t) : 0.0f, bias = writes && p.bias ? __ldg(p.bias + my_n) : 0.0f;
+    int sum[kRows][kOut] = {};
+    constexpr int kAhead = kRows * kOut >= 16 ? 2 : 8 / kOut;
+    for (int k0 = 16 * lane; k0 < p.k; k0 += 512 * kAhead) {
+        uint4 w[kAhead][kOut];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u)
+#pragma unroll
+            for (int o = 0; o < kOut; ++o) {
+                const int k = k0 + 512 * u;
+                w[u][o] = n0 + o < p.n ? load_codes(p.w + (int64_t)(n0 + o) * p.ldw + k, p.k - k) : make_uint4(0, 0, 0, 0);
+            }
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u)
+#pragma unroll
+            for (int t = 0; t < kRows; ++t) {
+                const int k = k0 + 512 * u;
+                const uint4 x = t < p.rows ? load_codes(p.x + (int64_t)t * p.ldx + k, p.k - k) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+                for (int o = 0; o < kOut; ++o) {
+                    int s = sum[t][o];
+                    s = __dp4a((int)x.x, (int)w[u][o].x, s);
+                    s = __dp4a((int)x.y, (int)w[u][o].y, s);
+                    s = __dp4a((int)x.z, (int)w[u][o].z, s);
+                    sum[t][o] = __dp4a((int)x.w, (int)w[u][o].w, s);
+                }
+            }
+    }
+#pragma unroll
+    for (int t = 0; t < kRows; ++t)
+#pragma unroll
+        for (int o = 0; o < kOut; ++o) sum[t][o] = __reduce_add_sync(0xffffffffu, sum[t][o]);
+    if (p.rank) conv::chain_wait();
+    float mine = 0.0f;                  // lane kOut t + o keeps that output
+    int my_id = -1;
+#pragma unroll
+    for (int t = 0; t < kRows; ++t) {
+        if (t >= p.rows) break;
+#pragma unroll
+        for (int o = 0; o < kOut; ++o) {
+            float outer = 0.0f;
+            if (p.rank && (unsigned)id[t] < (unsigned)p.n_adapters) {
+                for (int r = lane; r < p.rank; r += 32) {
+                    const uint32_t v = r < 32 ? b[t][o] : n0 + o < p.n ? __ldg(static_cast<const uint16_t *>(p.b) + ((int64_t)id[t] * p.n + n0 + o) * p.rank + r) : 0u;
+                    outer = fmaf(kHalf ? __half2float(__ushort_as_half((unsigned short)v)) : __uint_as_float(v << 16), p.inner[t * p.ranks + r], outer);
+                }
+#pragma unroll
+                for (int d = 16; d; d >>= 1) outer += __shfl_xor_sync(0xffffffffu, outer, d);
+            }
+            if (lane == kOut * t + o) {
+                mine = fmaf(w_scale, (float)sum[t][o], outer);
+                if (p.rank) my_id = id[t];
+            }
+        }
+    }
+    if (!writes) return;
+    mine = p.rank && my_id >= p.n_adapters ? NAN : fmaf(mine, x_scale, bias);
+    const int64_t at = (int64_t)my_t * p.ldy + my_n;
+    if (p.y_type == ISC_F32) static_cast<float *>(p.y)[at] = mine;
+    else if (p.y_type == ISC_F16) static_cast<__half *>(p.y)[at] = __float2half_rn(mine);
+    else static_cast<__nv_bfloat16 *>(p.y)[at] = __float2bfloat16_rn(mine);
 }
 
 // ---- the adapters' inner sums
@@ -540,7 +764,7 @@ struct InnerParams {
     bool vec_a;
 };
 
-constexpr int kInnerThreads = 256, kRankBlocks = 2;          // 32 ranks a block
+constexpr int kInnerThreads = 256;
 
 // four int8 as four 16-bit numbers, exactly
 template <bool kHalf> __device__ __forceinline__ uint2 widen(uint32_t v)
@@ -560,20 +784,9 @@ template <bool kHalf> __device__ __forceinline__ uint2 widen(uint32_t v)
     return make_uint2(*reinterpret_cast<const uint32_t *>(&a), *reinterpret_cast<const uint32_t *>(&b));
 }
 
-// sixteen codes of a row, zeros behind its end (which is read no further: it may be the tensor's)
-__device__ __forceinline__ uint4 load_codes(const int8_t *at, int left)
-{
-    if (left >= 16) return __ldg(reinterpret_cast<const uint4 *>(at));
-    uint32_t w[4] = {0, 0, 0, 0};
-#pragma unroll
-    for (int e = 0; e < 16; ++e)
-        if (e < left) w[e >> 2] |= (uint32_t)(uint8_t)at[e] << 8 * (e & 3);
-    return make_uint4(w[0], w[1], w[2], w[3]);
-}
-
-// kRowBlocks x 8 rows and 32 ranks for a block (a cluster where k is split): every warp takes one of the rows' adapters and a
+// kRowBlocks x 8 rows and kRankBlocks x 16 ranks for a block (a cluster where k is split): every warp takes one of the rows' adapters and a
 // part of k, ranks on the MMA's M side; the warps' sums meet in shared memory in a fixed order.
-template <bool kHalf, int kRowBlocks> __global__ void __launch_bounds__(kInnerThreads) k_adapter_rows(const __grid_constant__ InnerParams p)
+template <bool kHalf, int kRowBlocks, int kRankBlocks> __global__ void __launch_bounds__(kInnerThreads) k_adapter_rows(const __grid_constant__ InnerParams p)
 {
     constexpr int kRows = 8 * kRowBlocks, kWarps = kInnerThreads / 32, kRanks = 16 * kRankBlocks;
     __shared__ float4 sums[kWarps][kRankBlocks * kRowBlocks][32];
@@ -618,7 +831,8 @@ template <bool kHalf, int kRowBlocks> __global__ void __launch_bounds__(kInnerTh
                     ar[r][h] = rank < p.rank ? static_cast<const uint16_t *>(p.a) + ((int64_t)a * p.rank + rank) * p.k : nullptr;
                 }
             const int lo = chunk0 + (int)((int64_t)(chunk1 - chunk0) * share / shares), hi = chunk0 + (int)((int64_t)(chunk1 - chunk0) * (share + 1) / shares);
-#pragma unroll 2
+constexpr int kAhead = kRankBlocks * kRowBlocks == 1 ? 4 : 2;
+#pragma unroll kAhead
             for (int ch = lo; ch < hi; ++ch) {
                 const int k0 = 64 * ch + 16 * c;
                 uint4 xv[kRowBlocks];
@@ -701,27 +915,37 @@ bool encode_rows(void *encode, CUtensorMap *map, const int8_t *base, int64_t k, 
                               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// Row tile, and blocks that share a tile: tiles as even as they can be, and as many blocks at work as there are SMs.
+// Row tile, and blocks that share a tile: what takes the fewest cycles by a rough count.  A block of k costs 2.1 cycles for each
+// operand row; an epilogue 25 cycles a row and 50 more for every sixteen ranks (both measured at tiles of 256 rows), under the
+// next tile's products where there is one; starting, and joining the blocks that share a tile, a few thousand.
 void plan(LinearParams &p, int n_sms)
 {
     p.tiles_m = (p.n + kTileM - 1) / kTileM;
-    int64_t best = INT64_MAX;
     const int least = (p.rows + kMostTileN - 1) / kMostTileN;
-    for (int t = least; t <= std::min(2 * least + 1, least + 32); ++t) {
+    int64_t best = INT64_MAX;
+    for (int t = least; t <= std::min(4 * least + 4, least + 64); ++t) {
         const int width = ((p.rows + t - 1) / t + 15) & ~15, tiles_n = (p.rows + width - 1) / width;
-        const int64_t tiles = (int64_t)p.tiles_m * tiles_n, rounds = (tiles + n_sms - 1) / n_sms;
-        int split = 1;
-        while (split < kMostSplit && tiles * split * 2 <= n_sms && p.k_blocks >= 4 * split) split *= 2;
-        // operands delivered for a block of k, and a fixed share for a tile's start and end
-        const int64_t cost = rounds * ((int64_t)((p.k_blocks + split - 1) / split) * (width + kTileM) + 512 + 2 * width);
-        if (cost < best) {
-            best = cost;
-            p.tile_n = width;
-            p.tiles_n = tiles_n;
-            p.split = split;
+        // Narrow tiles are bound by W's bytes: two blocks to an SM, so that one's copies run under the other's start and end (16 rows,
+        // k = 8,192, n = 28,672: 49 us with one block and 192 KB of stages, 41 us with two and 80 KB each).
+        const bool narrow = width <= 64 && tiles_n == 1;
+        const int64_t tiles = (int64_t)p.tiles_m * tiles_n, slots = narrow ? 2 * n_sms : n_sms;
+        for (int split = 1; split <= kMostSplit && (split == 1 || (tiles * split <= slots && p.k_blocks >= 4 * split)); split *= 2) {
+            const bool part = narrow || split > 1;
+            const int64_t rounds = (tiles * split + slots - 1) / slots;
+            const double products = 2.1 * ((p.k_blocks + split - 1) / split) * (width + kTileM), end = (25.0 + 50.0 * (p.ranks >> 4)) * width / split + (split > 1 ? 2000.0 : 0.0);
+            const int64_t cost = (int64_t)(part ? rounds * (products + end + 3000.0) : rounds * std::max(products, end) + std::min(products, end) + 3000.0);
+            if (cost < best) {
+                best = cost;
+                p.tile_n = width;
+                p.tiles_n = tiles_n;
+                p.split = split;
+                p.form = part ? kPart : kTiles;
+                p.ring_bytes = narrow ? kRingBytesNarrow : kRingBytes;
+            }
         }
     }
-    p.stages = std::min<int>(kMostStages, kRingBytes / ((kTileM + p.tile_n) * kBlockK));
+    p.acc_stride = p.tile_n > 128 ? 256 : p.tile_n > 64 ? 128 : 64;
+    p.stages = std::min<int>(kMostStages, p.ring_bytes / ((kTileM + p.tile_n) * kBlockK));
 }
 
 template <typename P> cudaError_t launch(void (*kernel)(P), const P &p, dim3 grid, int threads, size_t smem, int cluster, bool chained, cudaStream_t st)
@@ -751,12 +975,13 @@ template <typename P> cudaError_t launch(void (*kernel)(P), const P &p, dim3 gri
 
 cudaError_t launch_inner(InnerParams p, int type, int n_sms, cudaStream_t st)
 {
-    const int row_blocks = p.rows >= 1024 ? 4 : 1;
-    const int64_t groups = (p.rows + 8 * row_blocks - 1) / (8 * row_blocks), ranks = (p.rank + 16 * kRankBlocks - 1) / (16 * kRankBlocks);
+    const int row_blocks = p.rows >= 1024 ? 4 : 1, rank_blocks = p.rank <= 16 ? 1 : 2;
+    const int64_t groups = (p.rows + 8 * row_blocks - 1) / (8 * row_blocks), ranks = (p.rank + 16 * rank_blocks - 1) / (16 * rank_blocks);
     p.split = 1;
-    while (p.split < kMostSplit && groups * ranks * p.split * 2 <= 2 * n_sms && p.k >= 64 * 16 * p.split) p.split *= 2;
-    void (*const kernel)(InnerParams) = type == ISC_F16 ? (row_blocks == 4 ? k_adapter_rows<true, 4> : k_adapter_rows<true, 1>) : (row_blocks == 4 ? k_adapter_rows<false, 4> : k_adapter_rows<false, 1>);
-    return launch(kernel, p, dim3((unsigned)(groups * p.split), (unsigned)ranks), kInnerThreads, 0, p.split, false, st);
+    while (p.split < kMostSplit && groups * ranks * p.split * 2 <= 2 * n_sms && p.k >= 64 * 8 * p.split) p.split *= 2;
+    void (*const kernels[2][2][2])(InnerParams) = {{{k_adapter_rows<false, 1, 1>, k_adapter_rows<false, 1, 2>}, {k_adapter_rows<false, 4, 1>, k_adapter_rows<false, 4, 2>}},
+                                                   {{k_adapter_rows<true, 1, 1>, k_adapter_rows<true, 1, 2>}, {k_adapter_rows<true, 4, 1>, k_adapter_rows<true, 4, 2>}}};
+    return launch(kernels[type == ISC_F16][row_blocks == 4][rank_blocks == 2], p, dim3((unsigned)(groups * p.split), (unsigned)ranks), kInnerThreads, 0, p.split, false, st);
 }
 
 }  // namespace
@@ -802,15 +1027,8 @@ extern "C" int isc_quant_linear(const int8_t *x, int64_t ldx, const float *x_sca
     p.y = y; p.ldy = ldy; p.y_type = y_type;
     p.rows = (int)rows; p.n = (int)n; p.k_blocks = (int)((k + kBlockK - 1) / kBlockK);
     p.vec_y = aligned(y, 16) && ldy * type_bytes(y_type) % 16 == 0;
-    plan(p, dev.n_sms);
-    if ((int64_t)p.tiles_m * p.tiles_n > INT32_MAX / kMostSplit) return ISC_ERR_UNSUPPORTED;
-    if (!dev.encode || !encode_rows(dev.encode, &p.map_w, w, k, n, ldw, kTileM) || !encode_rows(dev.encode, &p.map_x, x, k, rows, ldx, p.tile_n)) return ISC_ERR_CUDA;
     const cudaStream_t st = (cudaStream_t)cuda_stream;
-    const bool half = ad && ad->type == ISC_F16;
-    void (*const kernel)(LinearParams) = !ad ? k_quant_linear<-1, false> : ad->rank <= 16 ? (half ? k_quant_linear<1, true> : k_quant_linear<1, false>) :
-                                         ad->rank <= 32 ? (half ? k_quant_linear<2, true> : k_quant_linear<2, false>) : half ? k_quant_linear<0, true> : k_quant_linear<0, false>;
-    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem);
-    if (e != cudaSuccess) return status_of(e, "quant_linear");
+    const bool few = rows <= kFewRows, half = ad && ad->type == ISC_F16;
     if (ad) {
         InnerParams q = {};
         q.x = x; q.a = ad->a; q.scale = ad->scale; q.ids = ad->ids;
@@ -823,8 +1041,24 @@ extern "C" int isc_quant_linear(const int8_t *x, int64_t ldx, const float *x_sca
         p.b = ad->b; p.ids = ad->ids; p.inner = q.inner;
         p.rank = ad->rank; p.n_adapters = ad->n_adapters; p.adapter_type = ad->type;
     }
+    if (few) {
+        const FewParams f = {x, w, x_scale, w_scale, bias, p.inner, p.b, p.ids, y, ldx, ldw, ldy, p.rows, p.n, (int)k, p.rank, p.ranks, p.n_adapters, y_type};
+        void (*const kernel)(FewParams) = half ? k_quant_linear_few<1, 1, true> : k_quant_linear_few<1, 1, false>;
+        const int per_block = kFewThreads / 32;
+        e = launch(kernel, f, dim3((unsigned)((n + per_block - 1) / per_block)), kFewThreads, 0, 1, ad != nullptr, st);
+        return status_of(e, "quant_linear");
+    }
+    plan(p, dev.n_sms);
+    if ((int64_t)p.tiles_m * p.tiles_n > INT32_MAX / kMostSplit) return ISC_ERR_UNSUPPORTED;
+    if (!dev.encode || !encode_rows(dev.encode, &p.map_w, w, k, n, ldw, kTileM) || !encode_rows(dev.encode, &p.map_x, x, k, rows, ldx, p.tile_n)) return ISC_ERR_CUDA;
+    void (*const kernel)(LinearParams) =
+        p.form == kPart ? (!ad ? k_quant_linear<kPart, -1, false> : half ? k_quant_linear<kPart, 0, true> : k_quant_linear<kPart, 0, false>) :
+        !ad ? k_quant_linear<kTiles, -1, false> :
+        ad->rank <= 16 ? (half ? k_quant_linear<kTiles, 1, true> : k_quant_linear<kTiles, 1, false>) : half ? k_quant_linear<kTiles, 0, true> : k_quant_linear<kTiles, 0, false>;
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(kRingBytes + kSmemTiles));
+    if (e != cudaSuccess) return status_of(e, "quant_linear");
     const int tiles = p.tiles_m * p.tiles_n;
-    const unsigned grid = p.split > 1 ? (unsigned)(tiles * p.split) : (unsigned)std::min(tiles, dev.n_sms);
-    e = launch(kernel, p, dim3(grid), kThreads, kSmem, p.split, ad != nullptr, st);
+    const unsigned grid = p.form == kPart ? (unsigned)(tiles * p.split) : (unsigned)std::min(tiles, dev.n_sms);
+    e = launch(kernel, p, dim3(grid), kThreads, p.ring_bytes + (p.form == kPart ? kSmemPart : kSmemTiles), p.split, ad != nullptr, st);
     return status_of(e, "quant_linear");
 }

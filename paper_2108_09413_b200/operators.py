@@ -6,51 +6,58 @@ gradients: inputs that require one are refused while gradients are enabled.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes as C
 
-from .binding import IscError, _check, lib
+from .binding import IscError, lib
 
 _ARG = -1
+_torch = None                 # imported with the first call: the rest of the package works without it
+_types = {}
+
+
+def _start():
+    global _torch
+    import torch
+    _torch = torch
+    _types.update({torch.bfloat16: 0, torch.float16: 1, torch.float32: 2, torch.int8: 3})
+    return torch
 
 
 def _refuse(what, why):
     raise IscError(_ARG, f"{what}: {why}")
 
 
-def _type_code(t):
-    import torch
-    return {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2, torch.int8: 3}.get(t.dtype)
-
-
-def _tensors(what, first, *others):
-    """Every tensor is on the first one's GPU and needs no gradient."""
-    import torch
+def _same_device(what, tensors):
+    """The one GPU that all of the tensors (or None) are on; none of them may need a gradient."""
+    torch = _torch
+    first = tensors[0]
     if not isinstance(first, torch.Tensor) or not first.is_cuda:
         _refuse(what, "tensors have to be on a GPU")
-    grad = torch.is_grad_enabled()
-    for t in (first, *others):
-        if t is None:
-            continue
-        if not isinstance(t, torch.Tensor) or t.device != first.device:
-            _refuse(what, "tensors have to be on one GPU")
-        if grad and t.requires_grad:
-            _refuse(what, "no gradients are computed")
+    device, grad = first.device, torch.is_grad_enabled()
+    for t in tensors:
+        if t is not None:
+            if not isinstance(t, torch.Tensor) or t.device != device:
+                _refuse(what, "tensors have to be on one GPU")
+            if grad and t.requires_grad:
+                _refuse(what, "no gradients are computed")
+    return device
 
 
-def _matrix(what, name, t, dtype=None, shape=None):
+def _pitch(what, name, t, dtype=None, shape=None):
     """Pitch of a matrix whose rows' elements are adjacent."""
-    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+    own = t.shape
+    if len(own) != 2 or (own[1] > 1 and t.stride(1) != 1):
         _refuse(what, f"{name} has to be a matrix whose rows' elements are adjacent")
     if dtype is not None and t.dtype != dtype:
         _refuse(what, f"{name} has to be {dtype}")
-    if shape is not None and tuple(t.shape) != tuple(shape):
-        _refuse(what, f"{name} has to be {tuple(shape)}, not {tuple(t.shape)}")
-    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+    if shape is not None and own != shape:
+        _refuse(what, f"{name} has to be {tuple(shape)}, not {tuple(own)}")
+    ld = t.stride(0)
+    return ld if own[0] > 1 or ld > own[1] else own[1]
 
 
 def _vector(what, name, t, dtype, n):
-    if t is not None and (t.dim() != 1 or t.shape[0] != n or t.dtype != dtype or not t.is_contiguous()):
+    if t is not None and (t.dtype != dtype or t.shape != (n,) or not t.is_contiguous()):
         _refuse(what, f"{name} has to be {n} adjacent elements of {dtype}")
 
 
@@ -58,20 +65,22 @@ def _ptr(t):
     return t.data_ptr() if t is not None else None
 
 
-@contextlib.contextmanager
-def _on(device, stream):
-    import torch
-    with torch.cuda.device(device), (torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext()):
-        yield
+def _empty(shape, dtype, device):
+    # (torch.empty takes 0.9 us more)
+    return _torch.empty_strided(shape, (shape[1], 1) if len(shape) == 2 else (1,), dtype=dtype, device=device)
 
 
-def _enqueue(device, stream, call):
-    """`call(raw stream)` with the tensors' device and `stream` current."""
-    import torch
-    if stream is None and device.index == torch.cuda.current_device():
-        return call(torch.cuda.current_stream().cuda_stream)
-    with _on(device, stream):
-        return call(torch.cuda.current_stream(device).cuda_stream)
+def _enqueue(what, device, stream, call):
+    """`call(raw stream)`, a status, with the tensors' device and `stream` current."""
+    torch = _torch
+    index = device.index
+    if stream is None and index == torch.cuda.current_device():
+        rc = call(torch._C._cuda_getCurrentRawStream(index))
+    else:
+        with torch.cuda.device(index), torch.cuda.stream(stream if stream is not None else torch.cuda.current_stream(index)):
+            rc = call(torch._C._cuda_getCurrentRawStream(index))
+    if rc != 0:
+        raise IscError(rc, what)
 
 
 def rms_norm_quant(x, weight, eps=1e-6, residual=None, sum_out=None, stream=None):
@@ -82,32 +91,32 @@ def rms_norm_quant(x, weight, eps=1e-6, residual=None, sum_out=None, stream=None
     sum: x + residual in x's type, in `sum_out` where given (x or residual for in place); None without a residual and
     `sum_out`.  q's rows are 16 bytes aligned, as quant_linear takes them.
     """
-    import torch
+    torch = _torch or _start()
     what = "rms_norm_quant"
-    _tensors(what, x, weight, residual, sum_out)
-    code = _type_code(x)
-    if code is None or code == 3:
+    device = _same_device(what, (x, weight, residual, sum_out))
+    dtype, shape = x.dtype, x.shape
+    code = _types.get(dtype, 3)
+    if code == 3:
         _refuse(what, "x has to be bfloat16, float16 or float32")
-    ldx = _matrix(what, "x", x)
-    rows, width = x.shape
-    ldr = _matrix(what, "residual", residual, x.dtype, x.shape) if residual is not None else 0
-    if weight.dtype != torch.float32:
-        _vector(what, "weight", weight, x.dtype, width)
-    else:
-        _vector(what, "weight", weight, torch.float32, width)
+    ldx = _pitch(what, "x", x)
+    rows, width = shape
+    ldr = _pitch(what, "residual", residual, dtype, shape) if residual is not None else 0
+    wide = weight.dtype == torch.float32
+    _vector(what, "weight", weight, torch.float32 if wide else dtype, width)
+    if sum_out is not None:
+        _pitch(what, "sum_out", sum_out, dtype, shape)
+    pitch = (width + 15) & ~15
+    q = scale = total = None
 
     def call(raw):
-        total = sum_out
-        if total is None and residual is not None:
-            total = torch.empty((rows, width), dtype=x.dtype, device=x.device)
-        lds = _matrix(what, "sum_out", total, x.dtype, x.shape) if total is not None else 0
-        pitch = (width + 15) & ~15
-        q = torch.empty((rows, pitch), dtype=torch.int8, device=x.device)
-        scale = torch.empty(rows, dtype=torch.float32, device=x.device)
-        _check(lib().isc_rms_norm_quant(_ptr(x), ldx, _ptr(residual), ldr, _ptr(weight), _type_code(weight), code, rows, width, eps,
-                                        _ptr(total), lds, _ptr(q), pitch, _ptr(scale), raw), "isc_rms_norm_quant")
-        return (q if pitch == width else q[:, :width]), scale, total
-    return _enqueue(x.device, stream, call)
+        nonlocal q, scale, total
+        total = _empty(shape, dtype, device) if sum_out is None and residual is not None else sum_out
+        q = _empty((rows, pitch), torch.int8, device)
+        scale = _empty((rows,), torch.float32, device)
+        return lib().isc_rms_norm_quant(x.data_ptr(), ldx, _ptr(residual), ldr, weight.data_ptr(), 2 if wide else code, code, rows, width, eps,
+                                        _ptr(total), total.stride(0) if total is not None and rows > 1 else width, q.data_ptr(), pitch, scale.data_ptr(), raw)
+    _enqueue("isc_rms_norm_quant", device, stream, call)
+    return (q if pitch == width else q[:, :width]), scale, total
 
 
 class _Adapters(C.Structure):
@@ -124,11 +133,11 @@ def quant_linear(x, x_scale, w, w_scale, bias=None, adapters=None, adapter_ids=N
     adapter_ids: [rows] int32, negative for rows without one.  out_dtype: bfloat16 (the default), float16 or float32;
     `out`: where the result goes, any row pitch.
     """
-    import torch
+    torch = _torch or _start()
     what = "quant_linear"
     a, b, factor = adapters if adapters is not None else (None, None, None)
-    _tensors(what, x, x_scale, w, w_scale, bias, a, b, factor, adapter_ids, out)
-    ldx, ldw = _matrix(what, "x", x, torch.int8), _matrix(what, "w", w, torch.int8)
+    device = _same_device(what, (x, x_scale, w, w_scale, bias, a, b, factor, adapter_ids, out))
+    ldx, ldw = _pitch(what, "x", x, torch.int8), _pitch(what, "w", w, torch.int8)
     rows, k = x.shape
     n = w.shape[0]
     if w.shape[1] != k:
@@ -137,35 +146,40 @@ def quant_linear(x, x_scale, w, w_scale, bias=None, adapters=None, adapter_ids=N
     _vector(what, "w_scale", w_scale, torch.float32, n)
     _vector(what, "bias", bias, torch.float32, n)
     dtype = out.dtype if out is not None else out_dtype if out_dtype is not None else torch.bfloat16
-    if out is not None and out_dtype not in (None, out.dtype):
+    if out is not None and out_dtype not in (None, dtype):
         _refuse(what, "out is not of out_dtype")
-    code = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}.get(dtype)
-    if code is None:
+    code = _types.get(dtype, 3)
+    if code == 3:
         _refuse(what, "the result is bfloat16, float16 or float32")
+    if out is not None:
+        _pitch(what, "out", out, dtype, (rows, n))
     parts, space = None, 0
     if adapters is not None:
-        if a.dim() != 3 or b.dim() != 3 or a.dtype not in (torch.bfloat16, torch.float16) or b.dtype != a.dtype:
+        kind = _types.get(a.dtype, 3)
+        if kind > 1 or b.dtype != a.dtype or a.dim() != 3:
             _refuse(what, "adapters are bfloat16 or float16 [adapters, rank, k] and [adapters, n, rank]")
-        count, rank = a.shape[0], a.shape[1]
-        if a.shape[2] != k or tuple(b.shape) != (count, n, rank) or not a.is_contiguous() or not b.is_contiguous():
+        count, rank, depth = a.shape
+        if depth != k or b.shape != (count, n, rank) or not a.is_contiguous() or not b.is_contiguous():
             _refuse(what, f"adapters have to be {(count, rank, k)} and {(count, n, rank)} without gaps")
         _vector(what, "the adapters' scale", factor, torch.float32, count)
         if adapter_ids is None:
             _refuse(what, "adapters need adapter_ids")
         _vector(what, "adapter_ids", adapter_ids, torch.int32, rows)
         if count:
-            parts = _Adapters(_ptr(a), _ptr(b), _ptr(factor), _ptr(adapter_ids), _type_code(a), count, rank)
+            parts = _Adapters(a.data_ptr(), b.data_ptr(), factor.data_ptr(), adapter_ids.data_ptr(), kind, count, rank)
             space = ((rank + 15) // 16) * 64 * rows
+    y = out
 
     def call(raw):
-        y = torch.empty((rows, n), dtype=dtype, device=x.device) if out is None else out
-        ldy = _matrix(what, "out", y, dtype, (rows, n))
-        work = torch.empty(space, dtype=torch.uint8, device=x.device) if space else None
-        _check(lib().isc_quant_linear(_ptr(x), ldx, _ptr(x_scale), rows, _ptr(w), ldw, _ptr(w_scale), k, n, _ptr(bias),
-                                      C.addressof(parts) if parts is not None else None, _ptr(y), ldy, code, _ptr(work), space, raw),
-               "isc_quant_linear")
-        return y
-    return _enqueue(x.device, stream, call)
+        nonlocal y
+        if y is None:
+            y = _empty((rows, n), dtype, device)
+        work = _empty((space,), torch.uint8, device) if space else None
+        return lib().isc_quant_linear(x.data_ptr(), ldx, x_scale.data_ptr(), rows, w.data_ptr(), ldw, w_scale.data_ptr(), k, n, _ptr(bias),
+                                      C.addressof(parts) if parts is not None else None, y.data_ptr(), y.stride(0) if rows > 1 else n, code,
+                                      _ptr(work), space, raw)
+    _enqueue("isc_quant_linear", device, stream, call)
+    return y
 
 
 def log_probs(logits, targets=None, top=0, scale=1.0, votes=None, entropy=True, stream=None):
@@ -176,23 +190,29 @@ def log_probs(logits, targets=None, top=0, scale=1.0, votes=None, entropy=True, 
     probability is 0).  top: the number of alternatives, at most 32.  votes: [vocab] int32, to which 1 is added at every
     row's first alternative, as certify_decide and predict_decide take them (on the host).
     """
-    import torch
+    torch = _torch or _start()
     what = "log_probs"
-    _tensors(what, logits, targets, votes)
-    code = _type_code(logits)
+    device = _same_device(what, (logits, targets, votes))
+    code = _types.get(logits.dtype)
     if code is None:
         _refuse(what, "logits have to be bfloat16, float16, float32 or int8")
-    ld = _matrix(what, "logits", logits)
+    ld = _pitch(what, "logits", logits)
     rows, vocab = logits.shape
     _vector(what, "targets", targets, torch.int64, rows)
     _vector(what, "votes", votes, torch.int32, vocab)
+    given = h = ids = alternatives = None
 
     def call(raw):
-        given = torch.empty(rows, dtype=torch.float32, device=logits.device) if targets is not None else None
-        h = torch.empty(rows, dtype=torch.float32, device=logits.device) if entropy else None
-        ids = torch.empty((rows, top), dtype=torch.int32, device=logits.device) if top > 0 else None
-        alternatives = torch.empty((rows, top), dtype=torch.float32, device=logits.device) if top > 0 else None
-        _check(lib().isc_log_probs(_ptr(logits), ld, code, rows, vocab, scale, _ptr(targets), top, _ptr(given), _ptr(h), _ptr(ids),
-                                   _ptr(alternatives), _ptr(votes), raw), "isc_log_probs")
-        return given, h, ids, alternatives
-    return _enqueue(logits.device, stream, call)
+        nonlocal given, h, ids, alternatives
+        numbers = torch.float32
+        if targets is not None:
+            given = _empty((rows,), numbers, device)
+        if entropy:
+            h = _empty((rows,), numbers, device)
+        if top > 0:
+            ids = _empty((rows, top), torch.int32, device)
+            alternatives = _empty((rows, top), numbers, device)
+        return lib().isc_log_probs(logits.data_ptr(), ld, code, rows, vocab, scale, _ptr(targets), top, _ptr(given), _ptr(h), _ptr(ids),
+                                   _ptr(alternatives), _ptr(votes), raw)
+    _enqueue("isc_log_probs", device, stream, call)
+    return given, h, ids, alternatives
