@@ -2,7 +2,7 @@
 //
 //   z_i = scale (l_i - m),  S = sum exp(z),  log p_i = z_i - log S,  H = log S - sum(exp(z) z) / S
 //
-// One pass over a row: a thread takes every n-th chunk of eight logits and keeps its largest logit m, and S and
+// One pass over a row: a thread takes every n-th chunk of 16 bytes and keeps its largest logit m, and S and
 // U = sum exp(z) z relative to it, scaled again when a larger one comes; the threads' (m, S, U) are joined at the end.
 //
 // Alternatives without a second pass.  A thread's chunks are a subset of the row, and each of the row's k largest logits lies
@@ -11,8 +11,12 @@
 // out of the second-level cache: every logit not below the k-th maximum is a candidate, usually little more than k of them.
 // Order is by logit, then by lowest index, held as one 64-bit key, so ties are decided exactly.
 //
+// Three forms.  Many rows: persistent blocks, three to an SM, each with a ring of bulk copies that runs on into the next row while the
+// present one's threads join their sums and choose alternatives.  Few rows: a cluster of blocks for a row, joined through
+// its shared memory.  Short rows: a few lanes of a warp, the row in registers.
+//
 // Memory bound: 2 bytes a logit in bf16, one exponential each (11.6 logits a clock and SM at the copy bandwidth, of 16
-// exponentials).
+// exponentials); two-number instructions keep the rest below that.
 #include <cuda_runtime.h>
 #include <float.h>
 #include <math.h>
@@ -30,10 +34,12 @@ using namespace ops;
 
 constexpr int kMostTop = 32;
 constexpr int kThreads = 512;           // most threads of a block
-constexpr int kCandidates = 1024;
+constexpr int kCandidates = 512;
 constexpr int kMostCluster = 8;
 constexpr float kFloorZ = -150.0f;      // exp2 of it is zero in single precision
 typedef unsigned long long Key;
+
+__device__ int timeout_word;            // not zero: a bounded wait has run out
 
 struct LogProbParams {
     const void *logits;
@@ -114,54 +120,113 @@ __device__ __forceinline__ void write_alternative(const LogProbParams &p, const 
     p.top_log_probs[row * p.top + place] = r.bad ? NAN : some ? log_prob(p, r, logit) : -INFINITY;
 }
 
-// ---- a block, or a cluster of blocks, for a row
+// ---- long rows
 
-// A row in chunks of eight: chunk i holds elements 8 i - skew .. 8 i - skew + 7, so that whole chunks are aligned.
+// Sixteen bytes of a row.
+template <typename T> struct alignas(16) Chunk {
+    static constexpr int kSize = 16 / (int)sizeof(T);
+    T v[kSize];
+};
+__device__ __forceinline__ Pair pair_in(const Chunk<float> &c, int i) { return make_pair(c.v[2 * i], c.v[2 * i + 1]); }
+__device__ __forceinline__ Pair pair_in(const Chunk<__half> &c, int i)
+{
+    const float2 f = __half22float2(reinterpret_cast<const __half2 *>(&c)[i]);
+    return make_pair(f.x, f.y);
+}
+__device__ __forceinline__ Pair pair_in(const Chunk<__nv_bfloat16> &c, int i)
+{
+    const uint32_t w = reinterpret_cast<const uint32_t *>(&c)[i];
+    return make_pair(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u));
+}
+__device__ __forceinline__ Pair pair_in(const Chunk<int8_t> &c, int i) { return make_pair((float)c.v[2 * i], (float)c.v[2 * i + 1]); }
+
+// A row: whole aligned chunks, and up to 15 logits before the first and behind the last of them.
 template <typename T> struct Row {
     const T *at;
-    int vocab, skew, chunks;
+    int vocab, head, chunks;
     __device__ Row(const T *row, int v) : at(row), vocab(v)
     {
-        skew = (int)(((uintptr_t)row & (8 * sizeof(T) < 16 ? 7 : 15)) / sizeof(T));
-        chunks = (int)(((int64_t)vocab + skew + 7) >> 3);
+        head = (int)((0u - (uint32_t)(uintptr_t)row & 15u) / (uint32_t)sizeof(T));
+        chunks = (vocab - head) / Chunk<T>::kSize;
     }
-    __device__ __forceinline__ Eight<T> load(int chunk) const;
-    __device__ __forceinline__ bool whole(int chunk) const { return 8 * chunk >= skew && 8 * (int64_t)chunk - skew + 8 <= vocab; }
-    // element j of a chunk as a number, minus infinity outside the row
-    __device__ __forceinline__ float value(const Eight<T> &e, int chunk, int j) const
+    __device__ __forceinline__ const T *body() const { return at + head; }
+    __device__ __forceinline__ Chunk<T> load(int chunk) const
     {
-        const int64_t i = 8 * (int64_t)chunk - skew + j;
-        return i < 0 || i >= vocab ? -INFINITY : to_float(e.v[j]);
+        Chunk<T> c;
+        *reinterpret_cast<uint4 *>(&c) = __ldg(reinterpret_cast<const uint4 *>(body()) + chunk);
+        return c;
+    }
+    __device__ __forceinline__ int index(int chunk, int j) const { return head + chunk * Chunk<T>::kSize + j; }
+    // the logit outside the chunks that lane `lane` (0 .. 31) of one warp takes: its index, or -1
+    __device__ __forceinline__ int edge(int lane) const
+    {
+        const int i = lane < 16 ? lane : index(chunks, 0) + lane - 16;
+        return lane < 16 ? (i < head ? i : -1) : i < vocab ? i : -1;
     }
 };
-template <typename T> __device__ __forceinline__ Eight<T> Row<T>::load(int chunk) const
-{
-    const int64_t first = 8 * (int64_t)chunk - skew;
-    Eight<T> e;
-    if (whole(chunk)) {
-        if (sizeof(T) == 1) *reinterpret_cast<uint2 *>(&e) = __ldg(reinterpret_cast<const uint2 *>(at + first));
-        else {
+
+// A thread's part of a row.
+struct Own {
+    Sums sums{-INFINITY, 0.0f, 0.0f};
+    int best = 0;                       // the first chunk with the largest logit of its chunks
+    bool bad = false;
+    template <typename T> __device__ __forceinline__ void add(const Chunk<T> &e, int chunk, float c)
+    {
+        constexpr int kPairs = Chunk<T>::kSize / 2;
+        Pair x[kPairs];
+        float most = -INFINITY;
 #pragma unroll
-            for (unsigned w = 0; w < (sizeof(e) >= 16 ? sizeof(e) / 16 : 1); ++w) reinterpret_cast<uint4 *>(&e)[w] = __ldg(reinterpret_cast<const uint4 *>(at + first) + w);
+        for (int j = 0; j < kPairs; ++j) {
+            float a, b;
+            x[j] = pair_in(e, j);
+            split(x[j], a, b);
+            most = sizeof(T) == 1 ? max3(most, a, b) : max3_nan(most, a, b);
         }
-    } else {
+        if (sizeof(T) != 1) bad |= !(most < INFINITY);
+        if (most > sums.m) {
+            sums.scale_to(most, c);
+            best = chunk;
+        }
+        if (sums.m > -INFINITY) {
+            const Pair minus_m = make_pair(-sums.m, -sums.m), c2 = make_pair(c, c);
+            Pair s2 = make_pair(sums.s, 0.0f), u2 = make_pair(sums.u, 0.0f);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const int64_t i = first + j;
-            e.v[j] = at[i < 0 ? 0 : i >= vocab ? vocab - 1 : i];
+            for (int j = 0; j < kPairs; ++j) {
+                float a, b;
+                split(mul2(add2(x[j], minus_m), c2), a, b);
+                a = fmaxf(a, kFloorZ);
+                b = fmaxf(b, kFloorZ);
+                const Pair e2 = make_pair(exp2_fast(a), exp2_fast(b));
+                s2 = add2(s2, e2);
+                u2 = fma2(e2, make_pair(a, b), u2);
+            }
+            float a, b;
+            split(s2, a, b);
+            sums.s = a + b;
+            split(u2, a, b);
+            sums.u = a + b;
         }
     }
-    return e;
-}
+};
 
-struct Shared {
-    Sums warp[kThreads / 32];
+template <int kWarps> struct Shared {
+    Sums warp[kWarps];
     Sums block;                         // read by the cluster's other blocks
-    int bad, n_candidates;
-    Key sorted[kThreads / 32][32];
+    int bad[kWarps], block_bad, n_candidates;
+    Key sorted[kWarps][32];
     Key chosen[kMostTop];
     Key top[kMostTop];                  // read by the cluster's first block
     Key candidate[kCandidates];
+};
+
+// The threads that share a row, with a hardware barrier of their own.
+struct Team {
+    int t, threads, barrier;
+    __device__ __forceinline__ void sync() const
+    {
+        __syncwarp();
+        asm volatile("barrier.cta.sync.aligned %0, %1;" ::"r"(barrier), "r"(threads) : "memory");
+    }
 };
 
 __device__ __forceinline__ void cluster_sync()
@@ -183,25 +248,45 @@ __device__ __forceinline__ uint32_t read_remote(uint32_t addr)
     return v;
 }
 
-// Places of the `n` keys in `list` by counting the larger ones; the first `k` go to `top` (zero: none).
-__device__ void rank_candidates(Shared &sh, int n, int k, int t, int threads)
+// Every thread gets its team's sums.  `edge`: this thread's logit outside the chunks (minus infinity: none).
+template <int kWarps> __device__ __forceinline__ Sums join_all(Shared<kWarps> &sh, const Team &team, const Own &own, float edge, float c, bool &bad)
 {
-    if (t < kMostTop) sh.top[t] = 0;
-    __syncthreads();
-    for (int i = t; i < n; i += threads) {
+    Sums all = own.sums;
+    if (edge > -INFINITY) all = join(all, Sums{edge, 1.0f, 0.0f}, c);
+    bad = own.bad || edge != edge || edge == INFINITY;
+#pragma unroll
+    for (int d = 16; d; d >>= 1)
+        all = join(all, Sums{__shfl_xor_sync(0xffffffffu, all.m, d), __shfl_xor_sync(0xffffffffu, all.s, d), __shfl_xor_sync(0xffffffffu, all.u, d)}, c);
+    bad = __any_sync(0xffffffffu, bad) != 0;
+    if ((team.t & 31) == 0) { sh.warp[team.t >> 5] = all; sh.bad[team.t >> 5] = bad; }
+    if (team.t == 0) sh.n_candidates = 0;
+    team.sync();
+    all = sh.warp[0];
+    bad = sh.bad[0] != 0;
+    for (int w = 1; w < team.threads >> 5; ++w) { all = join(all, sh.warp[w], c); bad |= sh.bad[w] != 0; }
+    return all;
+}
+
+// Places of the `n` keys in `list` by counting the larger ones; the first `k` go to `top` (zero: none).
+template <int kWarps> __device__ void rank_candidates(Shared<kWarps> &sh, const Team &team, int n, int k)
+{
+    if (team.t < kMostTop) sh.top[team.t] = 0;
+    team.sync();
+    for (int i = team.t; i < n; i += team.threads) {
         const Key mine = sh.candidate[i];
         int place = 0;
         for (int j = 0; j < n; ++j) place += sh.candidate[j] > mine;
         if (place < k && mine) sh.top[place] = mine;
     }
-    __syncthreads();
+    team.sync();
 }
 
-// The k largest logits of this block's chunks into sh.top.
-template <typename T> __device__ void block_top(Shared &sh, const Row<T> &row, float m, int best, int first, int stride, int k, int t, int threads)
+// The k largest logits of this team's chunks and edges into sh.top; after join_all.  A thread's chunks are first, first + stride, ...
+template <typename T, int kWarps> __device__ void team_top(Shared<kWarps> &sh, const Team &team, const Row<T> &row, const Own &own, float edge, int edge_index, int first, int stride, int k)
 {
-    const int lane = t & 31, warp = t >> 5, warps = threads >> 5;
-    Key key = m > -INFINITY ? make_key(m, (uint32_t)best) : 0;
+    const int t = team.t, lane = t & 31, warp = t >> 5, warps = team.threads >> 5;
+    constexpr int kSize = Chunk<T>::kSize;
+    Key key = own.sums.m > -INFINITY ? make_key(own.sums.m, (uint32_t)own.best) : 0;
     // every warp sorts its threads' maxima, the largest first
 #pragma unroll
     for (int size = 2; size <= 32; size <<= 1) {
@@ -214,12 +299,11 @@ template <typename T> __device__ void block_top(Shared &sh, const Row<T> &row, f
     }
     sh.sorted[warp][lane] = key;
     if (t < kMostTop) sh.chosen[t] = 0;
-    if (t == 0) sh.n_candidates = 0;
-    __syncthreads();
+    team.sync();
     // its place among all: the larger ones of every other warp, by bisection (keys differ: their chunks do)
     if (lane < k && key) {
         int place = lane;
-        for (int w = 0; w < warps; ++w) {
+        for (int w = 0; w < warps && place < k; ++w) {
             if (w == warp) continue;
             int lo = 0, hi = min(k, 32);
             while (lo < hi) {
@@ -230,135 +314,66 @@ template <typename T> __device__ void block_top(Shared &sh, const Row<T> &row, f
         }
         if (place < k) sh.chosen[place] = key;
     }
-    __syncthreads();
+    if (edge > -INFINITY) {
+        const int at = atomicAdd(&sh.n_candidates, 1);
+        sh.candidate[at] = make_key(edge, (uint32_t)edge_index);     // (the first few: there is room)
+    }
+    team.sync();
     const Key least = sh.chosen[k - 1];
     for (int j = warp; j < k; j += warps) {
         const Key subset = sh.chosen[j];
         if (!subset) break;
         const int from = (int)(key_index(subset) % (uint32_t)stride);        // the subset's first chunk
         for (int i = from + lane * stride; i < row.chunks; i += 32 * stride) {
-            const Eight<T> e = row.load(i);
+            const Chunk<T> e = row.load(i);
 #pragma unroll
-            for (int q = 0; q < 8; ++q) {
-                const float v = row.value(e, i, q);
+            for (int q = 0; q < kSize; ++q) {
+                const float v = to_float(e.v[q]);
                 if (v > -INFINITY && make_key(v, (uint32_t)i) >= least) {
                     const int at = atomicAdd(&sh.n_candidates, 1);
-                    if (at < kCandidates) sh.candidate[at] = make_key(v, (uint32_t)(8 * i - row.skew + q));
+                    if (at < kCandidates) sh.candidate[at] = make_key(v, (uint32_t)row.index(i, q));
                 }
             }
         }
     }
-    __syncthreads();
+    team.sync();
     const int n = sh.n_candidates;
     if (n <= kCandidates) {
-        rank_candidates(sh, n, k, t, threads);
+        rank_candidates(sh, team, n, k);
         return;
     }
     // a row whose large logits all lie in a few subsets: one alternative after the other
     Key last = ~(Key)0;
     for (int r = 0; r < kMostTop; ++r) {
         Key found = 0;
-        if (r < k)
+        if (r < k) {
+            if (edge > -INFINITY && make_key(edge, (uint32_t)edge_index) < last) found = make_key(edge, (uint32_t)edge_index);
             for (int i = first; i < row.chunks; i += stride) {
-                const Eight<T> e = row.load(i);
+                const Chunk<T> e = row.load(i);
 #pragma unroll
-                for (int q = 0; q < 8; ++q) {
-                    const float v = row.value(e, i, q);
-                    const Key mine = v > -INFINITY ? make_key(v, (uint32_t)(8 * i - row.skew + q)) : 0;
+                for (int q = 0; q < kSize; ++q) {
+                    const float v = to_float(e.v[q]);
+                    const Key mine = v > -INFINITY ? make_key(v, (uint32_t)row.index(i, q)) : 0;
                     if (mine < last && mine > found) found = mine;
                 }
             }
+        }
 #pragma unroll
         for (int d = 16; d; d >>= 1) found = max(found, __shfl_xor_sync(0xffffffffu, found, d));
-        __syncthreads();
+        team.sync();
         if (lane == 0) sh.sorted[warp][0] = found;
-        __syncthreads();
+        team.sync();
         found = 0;
         for (int w = 0; w < warps; ++w) found = max(found, sh.sorted[w][0]);
         if (t == 0) sh.top[r] = found;
         last = found;
     }
-    __syncthreads();
+    team.sync();
 }
 
-template <typename T> __global__ void __launch_bounds__(kThreads) k_log_probs(const __grid_constant__ LogProbParams p)
+// by one thread for each alternative at least
+template <typename T, int kWarps> __device__ __forceinline__ void write_results(const LogProbParams &p, const Shared<kWarps> &sh, const Row<T> &row, int64_t row_index, Sums all, bool bad, int t)
 {
-    __shared__ Shared sh;
-    const int t = threadIdx.x, threads = blockDim.x, rank = p.cluster > 1 ? (int)(blockIdx.x % (unsigned)p.cluster) : 0;
-    const int64_t row_index = blockIdx.x / (unsigned)p.cluster;
-    const Row<T> row(static_cast<const T *>(p.logits) + row_index * p.ld, p.vocab);
-    const int stride = threads * p.cluster, first = rank * threads + t;
-    const float c = p.scale2;
-    Sums own{-INFINITY, 0.0f, 0.0f};
-    int best = 0;
-    bool bad = false;
-    constexpr int kAhead = 4;
-    for (int i0 = first; i0 < row.chunks; i0 += kAhead * stride) {
-        Eight<T> e[kAhead];
-#pragma unroll
-        for (int a = 0; a < kAhead; ++a)
-            if (i0 + a * stride < row.chunks) e[a] = row.load(i0 + a * stride);
-#pragma unroll
-        for (int a = 0; a < kAhead; ++a) {
-            const int i = i0 + a * stride;
-            if (i >= row.chunks) continue;
-            float x[8];
-            if (row.whole(i)) {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) x[j] = to_float(e[a].v[j]);
-            } else {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) x[j] = row.value(e[a], i, j);
-            }
-            float m = x[0];
-#pragma unroll
-            for (int j = 1; j < 8; ++j) m = sizeof(T) == 1 ? fmaxf(m, x[j]) : max_nan(m, x[j]);
-            if (sizeof(T) != 1) bad |= !(m < INFINITY);
-            if (m > own.m) {
-                own.scale_to(m, c);
-                best = i;
-            }
-            if (own.m > -INFINITY) {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const float z = fmaxf((x[j] - own.m) * c, kFloorZ), ez = exp2_fast(z);
-                    own.s += ez;
-                    own.u = fmaf(ez, z, own.u);
-                }
-            }
-        }
-    }
-    Sums all = own;
-#pragma unroll
-    for (int d = 16; d; d >>= 1)
-        all = join(all, Sums{__shfl_xor_sync(0xffffffffu, all.m, d), __shfl_xor_sync(0xffffffffu, all.s, d), __shfl_xor_sync(0xffffffffu, all.u, d)}, c);
-    if ((t & 31) == 0) sh.warp[t >> 5] = all;
-    bad = __syncthreads_or(bad) != 0;
-    all = sh.warp[0];
-    for (int w = 1; w < threads >> 5; ++w) all = join(all, sh.warp[w], c);
-    const int k = max(p.top, p.votes ? 1 : 0);
-    if (k) block_top<T>(sh, row, own.m, best, first, stride, k, t, threads);
-    if (p.cluster > 1) {
-        if (t == 0) { sh.block = all; sh.bad = bad; }
-        cluster_sync();
-        if (rank == 0) {
-            for (int b = 1; t < 32 && b < p.cluster; ++b) {      // the first warp writes the results
-                const uint32_t from = in_block(&sh.block, b);
-                all = join(all, Sums{__uint_as_float(read_remote(from)), __uint_as_float(read_remote(from + 4)), __uint_as_float(read_remote(from + 8))}, c);
-                bad |= read_remote(in_block(&sh.bad, b)) != 0;
-            }
-            if (k) {
-                for (int i = t; i < p.cluster * kMostTop; i += threads) {
-                    const uint32_t from = in_block(&sh.top[i % kMostTop], i / kMostTop);
-                    sh.candidate[i] = (Key)read_remote(from + 4) << 32 | read_remote(from);
-                }
-                __syncthreads();
-                rank_candidates(sh, p.cluster * kMostTop, k, t, threads);
-            }
-        }
-        cluster_sync();
-        if (rank) return;
-    }
     const RowResult r = row_result(all, bad);
     if (t == 0) write_row<T>(p, r, row.at, row_index);
     if (t < p.top) {
@@ -366,6 +381,123 @@ template <typename T> __global__ void __launch_bounds__(kThreads) k_log_probs(co
         write_alternative(p, r, row_index, t, key != 0, key_index(key), from_ordered((uint32_t)(key >> 32)));
     }
     if (p.votes && t == 0 && !bad && sh.top[0]) atomicAdd(p.votes + key_index(sh.top[0]), 1);
+}
+
+// few rows: a block or a cluster of them for a row
+template <typename T> __global__ void __launch_bounds__(kThreads) k_log_probs(const __grid_constant__ LogProbParams p)
+{
+    __shared__ Shared<kThreads / 32> sh;
+    const Team team{(int)threadIdx.x, (int)blockDim.x, 0};
+    const int t = team.t, threads = team.threads, rank = p.cluster > 1 ? (int)(blockIdx.x % (unsigned)p.cluster) : 0;
+    const int64_t row_index = blockIdx.x / (unsigned)p.cluster;
+    const Row<T> row(static_cast<const T *>(p.logits) + row_index * p.ld, p.vocab);
+    const int stride = threads * p.cluster, first = rank * threads + t, edge_index = rank == 0 && t < 32 ? row.edge(t) : -1;
+    const float c = p.scale2, edge = edge_index >= 0 ? to_float(row.at[edge_index]) : -INFINITY;
+    Own own;
+    constexpr int kAhead = 4;
+    for (int i0 = first; i0 < row.chunks; i0 += kAhead * stride) {
+        Chunk<T> e[kAhead];
+#pragma unroll
+        for (int a = 0; a < kAhead; ++a)
+            if (i0 + a * stride < row.chunks) e[a] = row.load(i0 + a * stride);
+#pragma unroll
+        for (int a = 0; a < kAhead; ++a)
+            if (i0 + a * stride < row.chunks) own.add(e[a], i0 + a * stride, c);
+    }
+    bool bad;
+    Sums all = join_all(sh, team, own, edge, c, bad);
+    const int k = max(p.top, p.votes ? 1 : 0);
+    if (k) team_top<T>(sh, team, row, own, edge, edge_index, first, stride, k);
+    if (p.cluster > 1) {
+        if (t == 0) { sh.block = all; sh.block_bad = bad; }
+        cluster_sync();
+        if (rank == 0) {
+            for (int b = 1; t < 32 && b < p.cluster; ++b) {      // the first warp writes the results
+                const uint32_t from = in_block(&sh.block, b);
+                all = join(all, Sums{__uint_as_float(read_remote(from)), __uint_as_float(read_remote(from + 4)), __uint_as_float(read_remote(from + 8))}, c);
+                bad |= read_remote(in_block(&sh.block_bad, b)) != 0;
+            }
+            if (k) {
+                for (int i = t; i < p.cluster * kMostTop; i += threads) {
+                    const uint32_t from = in_block(&sh.top[i % kMostTop], i / kMostTop);
+                    sh.candidate[i] = (Key)read_remote(from + 4) << 32 | read_remote(from);
+                }
+                team.sync();
+                rank_candidates(sh, team, p.cluster * kMostTop, k);
+            }
+        }
+        cluster_sync();
+        if (rank) return;
+    }
+    write_results(p, sh, row, row_index, all, bad, t);
+}
+
+// many rows: eight warps that work and one that copies
+constexpr int kStreamThreads = 256, kPieces = 8, kPieceBytes = 8192, kStreamBlocks = 3;
+template <typename T> __global__ void __launch_bounds__(kStreamThreads + 32, kStreamBlocks) k_log_probs_stream(const __grid_constant__ LogProbParams p)
+{
+    extern __shared__ __align__(128) uint8_t pieces[];
+    __shared__ Shared<kStreamThreads / 32> sh;
+    __shared__ __align__(8) uint64_t full[kPieces], empty[kPieces];
+    __shared__ int failed;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < kPieces; ++i) { tc::mbar_init(tc::smem_u32(&full[i]), 1); tc::mbar_init(tc::smem_u32(&empty[i]), kStreamThreads / 32); }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        failed = 0;
+    }
+    __syncthreads();
+    const T *logits = static_cast<const T *>(p.logits);
+    constexpr int kPieceChunks = kPieceBytes / 16;
+    int slot = 0, use = 0;
+    if (threadIdx.x >= kStreamThreads) {
+        if (threadIdx.x == kStreamThreads) {
+            int64_t issued = 0;
+            for (int64_t r = blockIdx.x; r < p.rows && !failed; r += gridDim.x) {
+                const Row<T> row(logits + r * p.ld, p.vocab);
+                for (int from = 0; from < row.chunks; from += kPieceChunks) {
+                    if (use && !wait_limited(tc::smem_u32(&empty[slot]), (uint32_t)(use - 1) & 1u, &failed)) { timeout_word = 1; break; }
+                    const uint32_t bytes = 16u * (uint32_t)min(kPieceChunks, row.chunks - from), bar = tc::smem_u32(&full[slot]);
+                    tc::mbar_expect_tx(bar, bytes);
+                    tc::bulk_g2s(tc::smem_u32(pieces + slot * kPieceBytes), reinterpret_cast<const uint8_t *>(row.body()) + 16 * (int64_t)from, bytes, bar);
+                    ++issued;
+                    if (++slot == kPieces) { slot = 0; ++use; }
+                }
+            }
+            // after a failure copies may still be under way
+            if (failed)
+                for (int64_t i = issued > kPieces ? issued - kPieces : 0; i < issued; ++i) {
+                    int again = 0;
+                    wait_limited(tc::smem_u32(&full[i % kPieces]), (uint32_t)(i / kPieces) & 1u, &again);
+                }
+        }
+        return;
+    }
+    const Team team{(int)threadIdx.x, kStreamThreads, 1};
+    const int t = team.t, k = max(p.top, p.votes ? 1 : 0);
+    const float c = p.scale2;
+    for (int64_t r = blockIdx.x; r < p.rows; r += gridDim.x) {
+        const Row<T> row(logits + r * p.ld, p.vocab);
+        const int edge_index = t < 32 ? row.edge(t) : -1;
+        const float edge = edge_index >= 0 ? to_float(row.at[edge_index]) : -INFINITY;
+        Own own;
+        for (int from = 0; from < row.chunks; from += kPieceChunks) {
+            if (!wait_limited(tc::smem_u32(&full[slot]), (uint32_t)use & 1u, &failed)) { timeout_word = 1; own.bad = true; }
+            const int here = min(kPieceChunks, row.chunks - from);
+#pragma unroll
+            for (int i = 0; i < kPieceChunks / kStreamThreads; ++i) {
+                const int at = i * kStreamThreads + t;
+                if (at < here) own.add(*reinterpret_cast<const Chunk<T> *>(pieces + slot * kPieceBytes + 16 * at), from + at, c);
+            }
+            __syncwarp();
+            if ((t & 31) == 0) tc::mbar_arrive(tc::smem_u32(&empty[slot]));
+            if (++slot == kPieces) { slot = 0; ++use; }
+        }
+        bool bad;
+        const Sums all = join_all(sh, team, own, edge, c, bad);
+        if (k) team_top<T>(sh, team, row, own, edge, edge_index, t, kStreamThreads, k);
+        write_results(p, sh, row, r, all, bad, t);
+        team.sync();
+    }
 }
 
 // ---- kLanes lanes of a warp for a row of at most kLanes x kHeld logits, which stay in registers
@@ -454,10 +586,16 @@ template <typename T> cudaError_t launch_log_probs(const Device &dev, LogProbPar
         else k_log_probs_group<T, 32, 32><<<grid, kGroupThreads, 0, st>>>(p);
         return cudaGetLastError();
     }
-    const int chunks = p.vocab / 8;
+    if (p.rows >= 2 * kStreamBlocks * dev.n_sms) {
+        const cudaError_t e = cudaFuncSetAttribute(k_log_probs_stream<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, kPieces * kPieceBytes);
+        if (e != cudaSuccess) return e;
+        k_log_probs_stream<T><<<(unsigned)(kStreamBlocks * dev.n_sms), kStreamThreads + 32, kPieces * kPieceBytes, st>>>(p);
+        return cudaGetLastError();
+    }
+    const int chunks = (int)(p.vocab * (int64_t)sizeof(T) / 16);
     const int threads = chunks >= 4 * kThreads ? kThreads : chunks >= 2 * kThreads ? kThreads / 2 : kThreads / 4;
     p.cluster = 1;
-    while (p.cluster < kMostCluster && p.rows * p.cluster * 2 <= 2 * dev.n_sms && chunks >= 4 * threads * p.cluster) p.cluster *= 2;
+    while (p.cluster < kMostCluster && p.rows * p.cluster * 2 <= 4 * dev.n_sms && chunks >= 4 * threads * p.cluster) p.cluster *= 2;
     cudaLaunchAttribute attr;
     attr.id = cudaLaunchAttributeClusterDimension;
     attr.val.clusterDim.x = (unsigned)p.cluster;
@@ -472,6 +610,10 @@ template <typename T> cudaError_t launch_log_probs(const Device &dev, LogProbPar
 }
 
 }  // namespace
+
+namespace ops {
+cudaError_t log_probs_take_timeout(cudaStream_t st, bool *expired) { return take_timeout(timeout_word, st, expired); }
+}  // namespace ops
 }  // namespace isc
 
 extern "C" int isc_log_probs(const void *logits, int64_t ld, int type, int64_t rows, int64_t vocab, float scale, const int64_t *targets, int top,

@@ -48,9 +48,10 @@ int status_of(cudaError_t e, const char *what)
 extern "C" int isc_operator_status(void *cuda_stream)
 {
     using namespace isc::ops;
-    bool norm = false, linear = false;
+    bool norm = false, linear = false, log_probs = false;
     cudaError_t e = norm_take_timeout((cudaStream_t)cuda_stream, &norm);
     if (e == cudaSuccess) e = linear_take_timeout((cudaStream_t)cuda_stream, &linear);
+    if (e == cudaSuccess) e = log_probs_take_timeout((cudaStream_t)cuda_stream, &log_probs);
     if (e != cudaSuccess) return status_of(e, "operator_status");
-    return norm || linear ? ISC_ERR_TIMEOUT : ISC_OK;
+    return norm || linear || log_probs ? ISC_ERR_TIMEOUT : ISC_OK;
 }

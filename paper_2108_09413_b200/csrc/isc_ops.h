@@ -24,6 +24,7 @@ cudaError_t current_device(Device *out);
 // Whether a bounded wait of the operators' kernels has run out on the current device since the last call; waits for `st`.
 cudaError_t norm_take_timeout(cudaStream_t st, bool *expired);
 cudaError_t linear_take_timeout(cudaStream_t st, bool *expired);
+cudaError_t log_probs_take_timeout(cudaStream_t st, bool *expired);
 
 // A failed CUDA call as a status; clears the runtime's sticky copy of the error.
 int status_of(cudaError_t e, const char *what);
