@@ -49,6 +49,7 @@ struct LogProbParams {
     int64_t rows, ld;
     int vocab, top, cluster;
     float scale, scale2;                // scale2 = scale log2(e)
+    float limit;                        // logits below it in magnitude take the short way
 };
 
 __device__ __forceinline__ float exp2_fast(float v)
@@ -165,46 +166,130 @@ template <typename T> struct Row {
     }
 };
 
-// A thread's part of a row.
-struct Own {
-    Sums sums{-INFINITY, 0.0f, 0.0f};
-    int best = 0;                       // the first chunk with the largest logit of its chunks
-    bool bad = false;
-    template <typename T> __device__ __forceinline__ void add(const Chunk<T> &e, int chunk, float c)
+// Masked logits as numbers that a product with zero leaves zero: minus infinity as the lowest finite number that the type's arithmetic
+// below can do without (kMasked), and whatever lies under it.
+template <typename T> struct Finite {
+    static constexpr float kMasked = -1e30f;
+    static __device__ __forceinline__ Chunk<T> of(Chunk<T> c) { return c; }
+};
+template <> struct Finite<__half> {
+    static constexpr float kMasked = -65504.0f;
+    static __device__ __forceinline__ Chunk<__half> of(Chunk<__half> c)
     {
-        constexpr int kPairs = Chunk<T>::kSize / 2;
-        Pair x[kPairs];
-        float most = -INFINITY;
 #pragma unroll
-        for (int j = 0; j < kPairs; ++j) {
-            float a, b;
-            x[j] = pair_in(e, j);
-            split(x[j], a, b);
-            most = sizeof(T) == 1 ? max3(most, a, b) : max3_nan(most, a, b);
-        }
-        if (sizeof(T) != 1) bad |= !(most < INFINITY);
-        if (most > sums.m) {
-            sums.scale_to(most, c);
-            best = chunk;
-        }
-        if (sums.m > -INFINITY) {
-            const Pair minus_m = make_pair(-sums.m, -sums.m), c2 = make_pair(c, c);
-            Pair s2 = make_pair(sums.s, 0.0f), u2 = make_pair(sums.u, 0.0f);
+        for (int j = 0; j < 4; ++j) asm("max.f16x2 %0, %0, %1;" : "+r"(reinterpret_cast<uint32_t *>(&c)[j]) : "r"(0xFBFFFBFFu));
+        return c;
+    }
+};
+template <> struct Finite<__nv_bfloat16> {
+    static constexpr float kMasked = -1.2676506e30f;     // -2^100
+    static __device__ __forceinline__ Chunk<__nv_bfloat16> of(Chunk<__nv_bfloat16> c)
+    {
 #pragma unroll
-            for (int j = 0; j < kPairs; ++j) {
-                float a, b;
-                split(mul2(add2(x[j], minus_m), c2), a, b);
-                a = fmaxf(a, kFloorZ);
-                b = fmaxf(b, kFloorZ);
-                const Pair e2 = make_pair(exp2_fast(a), exp2_fast(b));
-                s2 = add2(s2, e2);
-                u2 = fma2(e2, make_pair(a, b), u2);
-            }
+        for (int j = 0; j < 4; ++j) asm("max.bf16x2 %0, %0, %1;" : "+r"(reinterpret_cast<uint32_t *>(&c)[j]) : "r"(0xF180F180u));
+        return c;
+    }
+};
+template <> struct Finite<float> {
+    static constexpr float kMasked = -1e30f;
+    static __device__ __forceinline__ Chunk<float> of(Chunk<float> c)
+    {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) c.v[j] = fmaxf(c.v[j], kMasked);
+        return c;
+    }
+};
+
+template <typename T> __device__ __forceinline__ float largest(const Chunk<T> &e)
+{
+    float most = -INFINITY;
+#pragma unroll
+    for (int j = 0; j < Chunk<T>::kSize / 2; ++j) {
+        float a, b;
+        split(pair_in(e, j), a, b);
+        most = sizeof(T) == 1 ? max3(most, a, b) : max3_nan(most, a, b);
+    }
+    return most;
+}
+
+// A thread's part of a row.  Sums are kept as pairs, relative to m.
+struct Own {
+    float m = -INFINITY, seen = -INFINITY;      // seen: m, or NaN if there is one
+    Pair s = 0, u = 0;
+    int best = 0;                       // the first chunk with the largest logit of its chunks
+    __device__ __forceinline__ Sums sums() const
+    {
+        float a, b, x, y;
+        split(s, a, b);
+        split(u, x, y);
+        return Sums{m, a + b, x + y};
+    }
+    // a larger logit
+    __device__ __forceinline__ void rise(float to, float c)
+    {
+        Sums all = sums();
+        all.scale_to(to, c);
+        m = to;
+        s = make_pair(all.s, 0.0f);
+        u = make_pair(all.u, 0.0f);
+    }
+    // Logits between -1e30 and 1e29, but for masks, and factors below 1e8: no difference leaves single precision's range.
+    template <typename T> __device__ __forceinline__ void add_plain(const Chunk<T> &masked, Pair minus_m, Pair c2)
+    {
+        const Chunk<T> e = Finite<T>::of(masked);
+#pragma unroll
+        for (int j = 0; j < Chunk<T>::kSize / 2; ++j) {
             float a, b;
-            split(s2, a, b);
-            sums.s = a + b;
-            split(u2, a, b);
-            sums.u = a + b;
+            const Pair z = mul2(add2(pair_in(e, j), minus_m), c2);
+            split(z, a, b);
+            const Pair e2 = make_pair(exp2_fast(a), exp2_fast(b));
+            s = add2(s, e2);
+            u = fma2(e2, z, u);
+        }
+    }
+    // any logits
+    template <typename T> __device__ __noinline__ static void add_any(const Chunk<T> &e, float m, float c, Pair &s, Pair &u)
+    {
+        float sum = 0.0f, weighted = 0.0f;
+        for (int j = 0; j < Chunk<T>::kSize; ++j) {
+            const float z = fmaxf((to_float(e.v[j]) - m) * c, kFloorZ), ez = exp2_fast(z);
+            sum += ez;
+            weighted = fmaf(ez, z, weighted);
+        }
+        s = add2(s, make_pair(sum, 0.0f));
+        u = add2(u, make_pair(weighted, 0.0f));
+    }
+    // chunks first, first + stride, ...: `n` of them
+    template <typename T, int kN> __device__ __forceinline__ void add(const Chunk<T> (&e)[kN], int n, int first, int stride, float c, float limit)
+    {
+        float most[kN], all = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < kN; ++i) {
+            most[i] = i < n ? largest(e[i]) : -INFINITY;
+            all = sizeof(T) == 1 ? fmaxf(all, most[i]) : max_nan(all, most[i]);
+        }
+        if (sizeof(T) != 1) seen = max_nan(seen, all);
+        if (all > m) {
+            rise(all, c);
+#pragma unroll
+            for (int i = kN - 1; i >= 0; --i)
+                if (most[i] == all) best = first + i * stride;
+        }
+        if (m > (sizeof(T) == 2 ? Finite<T>::kMasked : -limit) && fabsf(m) < limit) {
+            const Pair minus_m = make_pair(-m, -m), c2 = make_pair(c, c);
+#pragma unroll
+            for (int i = 0; i < kN; ++i)
+                if (i < n) add_plain(e[i], minus_m, c2);
+        } else if (m > -INFINITY) {
+#pragma unroll
+            for (int i = 0; i < kN; ++i)
+                if (i < n) {
+                    Chunk<T> copy = e[i];
+                    Pair s_now = s, u_now = u;
+                    add_any(copy, m, c, s_now, u_now);
+                    s = s_now;
+                    u = u_now;
+                }
         }
     }
 };
@@ -251,9 +336,9 @@ __device__ __forceinline__ uint32_t read_remote(uint32_t addr)
 // Every thread gets its team's sums.  `edge`: this thread's logit outside the chunks (minus infinity: none).
 template <int kWarps> __device__ __forceinline__ Sums join_all(Shared<kWarps> &sh, const Team &team, const Own &own, float edge, float c, bool &bad)
 {
-    Sums all = own.sums;
+    Sums all = own.sums();
     if (edge > -INFINITY) all = join(all, Sums{edge, 1.0f, 0.0f}, c);
-    bad = own.bad || edge != edge || edge == INFINITY;
+    bad = !(own.seen < INFINITY) || edge != edge || edge == INFINITY;
 #pragma unroll
     for (int d = 16; d; d >>= 1)
         all = join(all, Sums{__shfl_xor_sync(0xffffffffu, all.m, d), __shfl_xor_sync(0xffffffffu, all.s, d), __shfl_xor_sync(0xffffffffu, all.u, d)}, c);
@@ -286,7 +371,7 @@ template <typename T, int kWarps> __device__ void team_top(Shared<kWarps> &sh, c
 {
     const int t = team.t, lane = t & 31, warp = t >> 5, warps = team.threads >> 5;
     constexpr int kSize = Chunk<T>::kSize;
-    Key key = own.sums.m > -INFINITY ? make_key(own.sums.m, (uint32_t)own.best) : 0;
+    Key key = own.m > -INFINITY ? make_key(own.m, (uint32_t)own.best) : 0;
     // every warp sorts its threads' maxima, the largest first
 #pragma unroll
     for (int size = 2; size <= 32; size <<= 1) {
@@ -400,9 +485,7 @@ template <typename T> __global__ void __launch_bounds__(kThreads) k_log_probs(co
 #pragma unroll
         for (int a = 0; a < kAhead; ++a)
             if (i0 + a * stride < row.chunks) e[a] = row.load(i0 + a * stride);
-#pragma unroll
-        for (int a = 0; a < kAhead; ++a)
-            if (i0 + a * stride < row.chunks) own.add(e[a], i0 + a * stride, c);
+        own.add(e, (row.chunks - i0 + stride - 1) / stride, i0, stride, c, p.limit);
     }
     bool bad;
     Sums all = join_all(sh, team, own, edge, c, bad);
@@ -433,7 +516,7 @@ template <typename T> __global__ void __launch_bounds__(kThreads) k_log_probs(co
 }
 
 // many rows: eight warps that work and one that copies
-constexpr int kStreamThreads = 256, kPieces = 8, kPieceBytes = 8192, kStreamBlocks = 3;
+constexpr int kStreamThreads = 256, kPieces = 4, kPieceBytes = 16384, kStreamBlocks = 3;
 template <typename T> __global__ void __launch_bounds__(kStreamThreads + 32, kStreamBlocks) k_log_probs_stream(const __grid_constant__ LogProbParams p)
 {
     extern __shared__ __align__(128) uint8_t pieces[];
@@ -481,13 +564,14 @@ template <typename T> __global__ void __launch_bounds__(kStreamThreads + 32, kSt
         const float edge = edge_index >= 0 ? to_float(row.at[edge_index]) : -INFINITY;
         Own own;
         for (int from = 0; from < row.chunks; from += kPieceChunks) {
-            if (!wait_limited(tc::smem_u32(&full[slot]), (uint32_t)use & 1u, &failed)) { timeout_word = 1; own.bad = true; }
-            const int here = min(kPieceChunks, row.chunks - from);
+            if (!wait_limited(tc::smem_u32(&full[slot]), (uint32_t)use & 1u, &failed)) { timeout_word = 1; own.seen = NAN; }
+            const int left = row.chunks - from - t;
+            constexpr int kN = kPieceChunks / kStreamThreads;
+            Chunk<T> e[kN];
 #pragma unroll
-            for (int i = 0; i < kPieceChunks / kStreamThreads; ++i) {
-                const int at = i * kStreamThreads + t;
-                if (at < here) own.add(*reinterpret_cast<const Chunk<T> *>(pieces + slot * kPieceBytes + 16 * at), from + at, c);
-            }
+            for (int i = 0; i < kN; ++i) e[i] = *reinterpret_cast<const Chunk<T> *>(pieces + slot * kPieceBytes + 16 * (i * kStreamThreads + t));
+            if (left > (kN - 1) * kStreamThreads) own.add(e, kN, from + t, kStreamThreads, c, p.limit);
+            else if (left > 0) own.add(e, (left + kStreamThreads - 1) / kStreamThreads, from + t, kStreamThreads, c, p.limit);
             __syncwarp();
             if ((t & 31) == 0) tc::mbar_arrive(tc::smem_u32(&empty[slot]));
             if (++slot == kPieces) { slot = 0; ++use; }
@@ -636,6 +720,7 @@ extern "C" int isc_log_probs(const void *logits, int64_t ld, int type, int64_t r
     p.rows = rows; p.ld = ld; p.vocab = (int)vocab; p.top = top; p.cluster = 1;
     p.scale = scale;
     p.scale2 = scale * 1.44269504088896f;
+    p.limit = p.scale2 < 1e8f ? 1e29f : 0.0f;
     const cudaStream_t st = (cudaStream_t)cuda_stream;
     e = type == ISC_BF16 ? launch_log_probs<__nv_bfloat16>(dev, p, st) : type == ISC_F16 ? launch_log_probs<__half>(dev, p, st) :
         type == ISC_F32 ? launch_log_probs<float>(dev, p, st) : launch_log_probs<int8_t>(dev, p, st);
