@@ -107,13 +107,21 @@ __device__ __forceinline__ float log_prob(const LogProbParams &p, const RowResul
 {
     return r.bad ? NAN : r.empty ? -INFINITY : (logit - r.m) * p.scale - r.log_s;
 }
-template <typename T> __device__ __forceinline__ void write_row(const LogProbParams &p, const RowResult &r, const T *row_logits, int64_t row)
+// A row's given token, loaded ahead of the row: two dependent loads that its end would wait for.
+struct Given { int64_t target; float logit; };
+template <typename T> __device__ __forceinline__ Given given_of(const LogProbParams &p, const T *row_logits, int64_t row, bool mine)
+{
+    Given g{-1, 0.0f};
+    if (mine && p.log_probs) {
+        g.target = p.targets[row];
+        if (g.target >= 0 && g.target < p.vocab) g.logit = to_float(row_logits[g.target]);
+    }
+    return g;
+}
+__device__ __forceinline__ void write_row(const LogProbParams &p, const RowResult &r, const Given &g, int64_t row)
 {
     if (p.entropy) p.entropy[row] = r.entropy;
-    if (p.log_probs) {
-        const int64_t target = p.targets[row];
-        p.log_probs[row] = target < 0 ? 0.0f : target >= p.vocab ? NAN : log_prob(p, r, to_float(row_logits[target]));
-    }
+    if (p.log_probs) p.log_probs[row] = g.target < 0 ? 0.0f : g.target >= p.vocab ? NAN : log_prob(p, r, g.logit);
 }
 __device__ __forceinline__ void write_alternative(const LogProbParams &p, const RowResult &r, int64_t row, int place, bool some, uint32_t index, float logit)
 {
@@ -297,20 +305,20 @@ struct Own {
 template <int kWarps> struct Shared {
     Sums warp[kWarps];
     Sums block;                         // read by the cluster's other blocks
-    int bad[kWarps], block_bad, n_candidates;
-    Key sorted[kWarps][32];
-    Key chosen[kMostTop];
+    int bad[kWarps], block_bad, n_candidates, n_chosen;
+    int chosen[32 * kWarps];            // first chunks of the subsets that hold the alternatives
+    Key group[32], found[kWarps];
     Key top[kMostTop];                  // read by the cluster's first block
-    Key candidate[kCandidates];
+    alignas(16) Key candidate[kCandidates];
 };
 
 // The threads that share a row, with a hardware barrier of their own.
 struct Team {
-    int t, threads, barrier;
+    int t, threads, barrier;            // barrier < 0: one warp
     __device__ __forceinline__ void sync() const
     {
         __syncwarp();
-        asm volatile("barrier.cta.sync.aligned %0, %1;" ::"r"(barrier), "r"(threads) : "memory");
+        if (barrier >= 0) asm volatile("barrier.cta.sync.aligned %0, %1;" ::"r"(barrier), "r"(threads) : "memory");
     }
 };
 
@@ -352,6 +360,23 @@ template <int kWarps> __device__ __forceinline__ Sums join_all(Shared<kWarps> &s
     return all;
 }
 
+// Place of the key at `lane` of list `own` among all of `lists` falling lists (at most eight), by bisection in all at once (keys differ).
+__device__ __forceinline__ void place_key(const Key (*sorted)[32], int lists, int own, int lane, Key key, int k, Key *out)
+{
+    if (lane >= k || !key) return;
+    int larger[kMostCluster] = {};
+#pragma unroll
+    for (int step = 16; step; step >>= 1)
+#pragma unroll
+        for (int w = 0; w < kMostCluster; ++w)
+            if (w < lists && sorted[w][larger[w] + step - 1] > key) larger[w] += step;
+    int place = lane;
+#pragma unroll
+    for (int w = 0; w < kMostCluster; ++w)
+        if (w < lists && w != own) place += larger[w] + (larger[w] == 31 && sorted[w][31] > key);
+    if (place < k) out[place] = key;
+}
+
 // Places of the `n` keys in `list` by counting the larger ones; the first `k` go to `top` (zero: none).
 template <int kWarps> __device__ void rank_candidates(Shared<kWarps> &sh, const Team &team, int n, int k)
 {
@@ -360,6 +385,7 @@ template <int kWarps> __device__ void rank_candidates(Shared<kWarps> &sh, const 
     for (int i = team.t; i < n; i += team.threads) {
         const Key mine = sh.candidate[i];
         int place = 0;
+#pragma unroll 8
         for (int j = 0; j < n; ++j) place += sh.candidate[j] > mine;
         if (place < k && mine) sh.top[place] = mine;
     }
@@ -371,52 +397,47 @@ template <typename T, int kWarps> __device__ void team_top(Shared<kWarps> &sh, c
 {
     const int t = team.t, lane = t & 31, warp = t >> 5, warps = team.threads >> 5;
     constexpr int kSize = Chunk<T>::kSize;
-    Key key = own.m > -INFINITY ? make_key(own.m, (uint32_t)own.best) : 0;
-    // every warp sorts its threads' maxima, the largest first
-#pragma unroll
-    for (int size = 2; size <= 32; size <<= 1) {
-#pragma unroll
-        for (int d = size >> 1; d; d >>= 1) {
-            const Key other = __shfl_xor_sync(0xffffffffu, key, d);
-            const bool keep_larger = ((lane & d) == 0) == ((lane & size) == 0 || size == 32);
-            key = (key > other) == keep_larger ? key : other;
-        }
-    }
-    sh.sorted[warp][lane] = key;
-    if (t < kMostTop) sh.chosen[t] = 0;
+    const Key key = own.m > -INFINITY ? make_key(own.m, (uint32_t)own.best) : 0;
+    // The k-th largest of 32 groups' largest keys: k subsets at least reach it, and seldom many more (all of a warp's lanes
+    // are a group each, k exactly).  A full order of the subsets' maxima took 1.5 us here.
+    const int group = team.threads >> 5;
+    Key most = key;
+    for (int d = 1; d < group; d <<= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, d));
+    if ((t & (group - 1)) == 0) sh.group[t / group] = most;
+    if (t == 0) sh.n_chosen = 0;
     team.sync();
-    // its place among all: the larger ones of every other warp, by bisection (keys differ: their chunks do)
-    if (lane < k && key) {
-        int place = lane;
-        for (int w = 0; w < warps && place < k; ++w) {
-            if (w == warp) continue;
-            int lo = 0, hi = min(k, 32);
-            while (lo < hi) {
-                const int mid = (lo + hi) >> 1;
-                if (sh.sorted[w][mid] > key) lo = mid + 1; else hi = mid;
-            }
-            place += lo;
-        }
-        if (place < k) sh.chosen[place] = key;
-    }
+    most = sh.group[lane];
+    int larger = 0;
+#pragma unroll 8
+    for (int j = 0; j < 32; ++j) larger += sh.group[j] > most;
+    const uint32_t kth = __ballot_sync(0xffffffffu, most && larger == k - 1);
+    const Key least = kth ? __shfl_sync(0xffffffffu, most, __ffs((int)kth) - 1) : 1;
+    if (key >= least) sh.chosen[atomicAdd(&sh.n_chosen, 1)] = first;
     if (edge > -INFINITY) {
         const int at = atomicAdd(&sh.n_candidates, 1);
         sh.candidate[at] = make_key(edge, (uint32_t)edge_index);     // (the first few: there is room)
     }
     team.sync();
-    const Key least = sh.chosen[k - 1];
-    for (int j = warp; j < k; j += warps) {
-        const Key subset = sh.chosen[j];
-        if (!subset) break;
-        const int from = (int)(key_index(subset) % (uint32_t)stride);        // the subset's first chunk
-        for (int i = from + lane * stride; i < row.chunks; i += 32 * stride) {
-            const Chunk<T> e = row.load(i);
+    // the chosen subsets' chunks, dealt out over all threads, four loads of a thread under way at once
+    const int each = (row.chunks + stride - 1) / stride, items = sh.n_chosen * each;
+    for (int i0 = t; i0 < items; i0 += 4 * team.threads) {
+        Chunk<T> e[4];
+        int chunk[4];
+#pragma unroll
+        for (int a = 0; a < 4; ++a) {
+            const int i = i0 + a * team.threads, j = i / each;
+            chunk[a] = i < items ? sh.chosen[j] + (i - j * each) * stride : row.chunks;
+            if (chunk[a] < row.chunks) e[a] = row.load(chunk[a]);
+        }
+#pragma unroll
+        for (int a = 0; a < 4; ++a) {
+            if (chunk[a] >= row.chunks) continue;
 #pragma unroll
             for (int q = 0; q < kSize; ++q) {
-                const float v = to_float(e.v[q]);
-                if (v > -INFINITY && make_key(v, (uint32_t)i) >= least) {
+                const float v = to_float(e[a].v[q]);
+                if (v > -INFINITY && make_key(v, (uint32_t)chunk[a]) >= least) {
                     const int at = atomicAdd(&sh.n_candidates, 1);
-                    if (at < kCandidates) sh.candidate[at] = make_key(v, (uint32_t)row.index(i, q));
+                    if (at < kCandidates) sh.candidate[at] = make_key(v, (uint32_t)row.index(chunk[a], q));
                 }
             }
         }
@@ -446,10 +467,10 @@ template <typename T, int kWarps> __device__ void team_top(Shared<kWarps> &sh, c
 #pragma unroll
         for (int d = 16; d; d >>= 1) found = max(found, __shfl_xor_sync(0xffffffffu, found, d));
         team.sync();
-        if (lane == 0) sh.sorted[warp][0] = found;
+        if (lane == 0) sh.found[warp] = found;
         team.sync();
         found = 0;
-        for (int w = 0; w < warps; ++w) found = max(found, sh.sorted[w][0]);
+        for (int w = 0; w < warps; ++w) found = max(found, sh.found[w]);
         if (t == 0) sh.top[r] = found;
         last = found;
     }
@@ -457,10 +478,10 @@ template <typename T, int kWarps> __device__ void team_top(Shared<kWarps> &sh, c
 }
 
 // by one thread for each alternative at least
-template <typename T, int kWarps> __device__ __forceinline__ void write_results(const LogProbParams &p, const Shared<kWarps> &sh, const Row<T> &row, int64_t row_index, Sums all, bool bad, int t)
+template <int kWarps> __device__ __forceinline__ void write_results(const LogProbParams &p, const Shared<kWarps> &sh, const Given &given, int64_t row_index, Sums all, bool bad, int t)
 {
     const RowResult r = row_result(all, bad);
-    if (t == 0) write_row<T>(p, r, row.at, row_index);
+    if (t == 0) write_row(p, r, given, row_index);
     if (t < p.top) {
         const Key key = sh.top[t];
         write_alternative(p, r, row_index, t, key != 0, key_index(key), from_ordered((uint32_t)(key >> 32)));
@@ -478,6 +499,7 @@ template <typename T> __global__ void __launch_bounds__(kThreads) k_log_probs(co
     const Row<T> row(static_cast<const T *>(p.logits) + row_index * p.ld, p.vocab);
     const int stride = threads * p.cluster, first = rank * threads + t, edge_index = rank == 0 && t < 32 ? row.edge(t) : -1;
     const float c = p.scale2, edge = edge_index >= 0 ? to_float(row.at[edge_index]) : -INFINITY;
+    const Given given = given_of(p, row.at, row_index, rank == 0 && t == 0);
     Own own;
     constexpr int kAhead = 4;
     for (int i0 = first; i0 < row.chunks; i0 += kAhead * stride) {
@@ -501,18 +523,55 @@ template <typename T> __global__ void __launch_bounds__(kThreads) k_log_probs(co
                 bad |= read_remote(in_block(&sh.block_bad, b)) != 0;
             }
             if (k) {
-                for (int i = t; i < p.cluster * kMostTop; i += threads) {
-                    const uint32_t from = in_block(&sh.top[i % kMostTop], i / kMostTop);
-                    sh.candidate[i] = (Key)read_remote(from + 4) << 32 | read_remote(from);
+                Key (*const sorted)[32] = reinterpret_cast<Key (*)[32]>(sh.candidate);
+                const int list = t / kMostTop, lane = t % kMostTop;
+                Key key = 0;
+                if (list < p.cluster) {
+                    const uint32_t from = in_block(&sh.top[lane], list);
+                    key = (Key)read_remote(from + 4) << 32 | read_remote(from);
+                    sorted[list][lane] = key;
                 }
                 team.sync();
-                rank_candidates(sh, team, p.cluster * kMostTop, k);
+                if (t < kMostTop) sh.top[t] = 0;             // (this block's own list has been copied)
+                team.sync();
+                if (list < p.cluster) place_key(sorted, p.cluster, list, lane, key, k, sh.top);
+                team.sync();
             }
         }
         cluster_sync();
         if (rank) return;
     }
-    write_results(p, sh, row, row_index, all, bad, t);
+    write_results(p, sh, given, row_index, all, bad, t);
+}
+
+// rows of middling length: a warp for a row
+constexpr int kRowWarps = 4;
+template <typename T> __global__ void __launch_bounds__(32 * kRowWarps) k_log_probs_warp(const __grid_constant__ LogProbParams p)
+{
+    __shared__ Shared<1> shared[kRowWarps];
+    Shared<1> &sh = shared[threadIdx.x >> 5];
+    const Team team{(int)threadIdx.x & 31, 32, -1};
+    const int t = team.t, k = max(p.top, p.votes ? 1 : 0);
+    const float c = p.scale2;
+    const int64_t r = (int64_t)blockIdx.x * kRowWarps + (threadIdx.x >> 5);
+    if (r >= p.rows) return;
+    const Row<T> row(static_cast<const T *>(p.logits) + r * p.ld, p.vocab);
+    const int edge_index = row.edge(t);
+    const float edge = edge_index >= 0 ? to_float(row.at[edge_index]) : -INFINITY;
+    const Given given = given_of(p, row.at, r, t == 0);
+    Own own;
+    constexpr int kAhead = 4;
+    for (int i0 = t; i0 < row.chunks; i0 += 32 * kAhead) {
+        Chunk<T> e[kAhead];
+#pragma unroll
+        for (int a = 0; a < kAhead; ++a)
+            if (i0 + a * 32 < row.chunks) e[a] = row.load(i0 + a * 32);
+        own.add(e, (row.chunks - i0 + 31) / 32, i0, 32, c, p.limit);
+    }
+    bool bad;
+    const Sums all = join_all(sh, team, own, edge, c, bad);
+    if (k) team_top<T>(sh, team, row, own, edge, edge_index, t, 32, k);
+    write_results(p, sh, given, r, all, bad, t);
 }
 
 // many rows: eight warps that work and one that copies
@@ -562,6 +621,7 @@ template <typename T> __global__ void __launch_bounds__(kStreamThreads + 32, kSt
         const Row<T> row(logits + r * p.ld, p.vocab);
         const int edge_index = t < 32 ? row.edge(t) : -1;
         const float edge = edge_index >= 0 ? to_float(row.at[edge_index]) : -INFINITY;
+        const Given given = given_of(p, row.at, r, t == 0);
         Own own;
         for (int from = 0; from < row.chunks; from += kPieceChunks) {
             if (!wait_limited(tc::smem_u32(&full[slot]), (uint32_t)use & 1u, &failed)) { timeout_word = 1; own.seen = NAN; }
@@ -570,8 +630,14 @@ template <typename T> __global__ void __launch_bounds__(kStreamThreads + 32, kSt
             Chunk<T> e[kN];
 #pragma unroll
             for (int i = 0; i < kN; ++i) e[i] = *reinterpret_cast<const Chunk<T> *>(pieces + slot * kPieceBytes + 16 * (i * kStreamThreads + t));
-            if (left > (kN - 1) * kStreamThreads) own.add(e, kN, from + t, kStreamThreads, c, p.limit);
-            else if (left > 0) own.add(e, (left + kStreamThreads - 1) / kStreamThreads, from + t, kStreamThreads, c, p.limit);
+            if (left > (kN - 1) * kStreamThreads && sizeof(T) > 1) own.add(e, kN, from + t, kStreamThreads, c, p.limit);
+            else if (sizeof(T) == 1) {
+#pragma unroll 1
+                for (int i = 0; i < kN && left > i * kStreamThreads; ++i) {
+                    const Chunk<T> one[1] = {*reinterpret_cast<const Chunk<T> *>(pieces + slot * kPieceBytes + 16 * (i * kStreamThreads + t))};
+                    own.add(one, 1, from + i * kStreamThreads + t, kStreamThreads, c, p.limit);
+                }
+            } else if (left > 0) own.add(e, (left + kStreamThreads - 1) / kStreamThreads, from + t, kStreamThreads, c, p.limit);
             __syncwarp();
             if ((t & 31) == 0) tc::mbar_arrive(tc::smem_u32(&empty[slot]));
             if (++slot == kPieces) { slot = 0; ++use; }
@@ -579,7 +645,7 @@ template <typename T> __global__ void __launch_bounds__(kStreamThreads + 32, kSt
         bool bad;
         const Sums all = join_all(sh, team, own, edge, c, bad);
         if (k) team_top<T>(sh, team, row, own, edge, edge_index, t, kStreamThreads, k);
-        write_results(p, sh, row, r, all, bad, t);
+        write_results(p, sh, given, r, all, bad, t);
         team.sync();
     }
 }
@@ -603,6 +669,7 @@ template <typename T, int kLanes, int kHeld> __global__ void __launch_bounds__(k
         const int64_t row_index = row0 + threadIdx.x / kLanes;
         const bool mine = row_index < p.rows;
         const T *row = static_cast<const T *>(p.logits) + (mine ? row_index : p.rows - 1) * p.ld;
+        const Given given = given_of(p, row, row_index, mine && lane == 0);
         float x[kHeld];
         float m = -INFINITY;
 #pragma unroll
@@ -628,7 +695,7 @@ template <typename T, int kLanes, int kHeld> __global__ void __launch_bounds__(k
             all.u += __shfl_xor_sync(0xffffffffu, all.u, d);
         }
         const RowResult r = row_result(all, bad);
-        if (mine && lane == 0) write_row<T>(p, r, row, row_index);
+        if (mine && lane == 0) write_row(p, r, given, row_index);
         const int k = max(p.top, p.votes ? 1 : 0);
         uint32_t used = 0;
         for (int place = 0; place < k; ++place) {
@@ -662,12 +729,17 @@ template <typename T, int kLanes, int kHeld> __global__ void __launch_bounds__(k
 
 template <typename T> cudaError_t launch_log_probs(const Device &dev, LogProbParams p, cudaStream_t st)
 {
-    if (p.vocab <= 1024) {
-        const bool narrow = p.vocab <= 64;
-        const int64_t per_block = kGroupThreads / (narrow ? 8 : 32);
+    if (p.vocab <= 64) {
+        const int lanes = p.vocab <= 16 ? 1 : 8;
+        const int64_t per_block = kGroupThreads / lanes;
         const unsigned grid = (unsigned)std::min<int64_t>((p.rows + per_block - 1) / per_block, 8 * dev.n_sms);
-        if (narrow) k_log_probs_group<T, 8, 8><<<grid, kGroupThreads, 0, st>>>(p);
-        else k_log_probs_group<T, 32, 32><<<grid, kGroupThreads, 0, st>>>(p);
+        if (lanes == 1) k_log_probs_group<T, 1, 16><<<grid, kGroupThreads, 0, st>>>(p);
+        else k_log_probs_group<T, 8, 8><<<grid, kGroupThreads, 0, st>>>(p);
+        return cudaGetLastError();
+    }
+    // (a warp takes 16 chunks a lane in the time that a block's barriers take)
+    if (p.vocab <= 4096 || (p.vocab <= 16384 && p.rows >= 16 * dev.n_sms)) {
+        k_log_probs_warp<T><<<(unsigned)((p.rows + kRowWarps - 1) / kRowWarps), 32 * kRowWarps, 0, st>>>(p);
         return cudaGetLastError();
     }
     if (p.rows >= 2 * kStreamBlocks * dev.n_sms) {
