@@ -46,8 +46,19 @@ constexpr int kMostStages = 12, kMostTileN = 256, kMostSplit = 8;
 constexpr uint32_t kRingBytes = 192 * 1024, kRingBytesNarrow = 96 * 1024;
 constexpr uint32_t kStageRow = 80, kStageRowWide = 144;      // bytes from row to row of a warp's output staging (16-bit, 32-bit)
 constexpr uint32_t kStaging = 8 * kStageRowWide;
-constexpr uint32_t kInnerRow = 80, kInnerStage = 16 * kInnerRow;      // sixteen rows' inner sums of sixteen ranks, rows apart so that four of them are read at once
-constexpr size_t kSmemPart = kEpilogueWarps * kStaging + 1024, kSmemTiles = kSmemPart + kEpilogueWarps * 2 * kInnerStage;   // beside the stages
+constexpr size_t kSmemBeside = kEpilogueWarps * kStaging + 1024;       // beside the stages
+constexpr size_t kSmemMost = 231936;
+// A tile's inner sums, and its adapter's B, in shared memory: bytes from row to row and from output to output, so that the four rows and the
+// eight outputs that a warp reads at once lie in different banks.
+__host__ __device__ constexpr uint32_t inner_pitch(int ranks) { return (uint32_t)ranks * 4u + 16u; }
+__host__ __device__ constexpr uint32_t left_pitch(int ranks) { return (uint32_t)ranks * 2u + 8u; }
+// the widest tile that leaves them room beside four stages
+constexpr int widest_tile(int ranks)
+{
+    int width = kMostTileN;
+    while (width > 16 && (size_t)(4 * (kTileM + width) * kBlockK) + kSmemBeside + (ranks ? width * inner_pitch(ranks) + kTileM * left_pitch(ranks) : 0) > kSmemMost) width -= 16;
+    return width;
+}
 
 enum Form { kTiles, kPart };
 
@@ -119,6 +130,13 @@ __device__ __forceinline__ int read_remote(uint32_t addr)
     return v;
 }
 
+// the epilogue's warps
+__device__ __forceinline__ void epilogue_sync()
+{
+    __syncwarp();
+    asm volatile("barrier.cta.sync.aligned 1, %0;" ::"n"(32 * kEpilogueWarps) : "memory");
+}
+
 // What a warp's lane needs for its four outputs of a 32-output strip: fragment rows lane / 4 + 8 i.
 struct Strip {
     int n0;
@@ -166,6 +184,13 @@ struct Left {
                 v[i][q] = 16 * block + 4 * q < p.rank && n0 + (lane >> 2) + 8 * i < p.n ? __ldg(reinterpret_cast<const uint2 *>(b + (int64_t)8 * i * p.rank + 4 * q)) : make_uint2(0, 0);
     }
 };
+__device__ __forceinline__ void load_kept(Left &left, const uint8_t *kept, uint32_t pitch, int block, int lane)
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) left.v[i][q] = *reinterpret_cast<const uint2 *>(kept + (uint32_t)((lane >> 2) + 8 * i) * pitch + (uint32_t)(32 * block + 8 * q));
+}
 template <bool kHalf> __device__ __forceinline__ Pair widen_pair(uint32_t w)
 {
     if (kHalf) {
@@ -424,16 +449,13 @@ __device__ __forceinline__ void prefetch_adapters(const LinearParams &p, int n0,
 
 // kForm kTiles: persistent blocks with tile after tile.  kPart: a tile, or a part of k of one, for a block, two blocks to an SM if
 // the tile is narrow.
-// kHeld: 1: up to sixteen ranks, of which B stays in registers from rows to rows; 0: more, loaded for every sixteen rows (two blocks
-// in registers, which spill a little then: 246 us against 209 at 8,192 rows, k = n = 4,096, rank 32); -1: no adapters.
-template <Form kForm, int kHeld, bool kHalf> __global__ void __launch_bounds__(kThreads, kForm == kPart ? 2 : 1) k_quant_linear(const __grid_constant__ LinearParams p)
+template <Form kForm, bool kAdapters, bool kHalf> __global__ void __launch_bounds__(kThreads, kForm == kPart ? 2 : 1) k_quant_linear(const __grid_constant__ LinearParams p)
 {
     extern __shared__ uint8_t smem_raw[];
     __shared__ __align__(8) uint64_t bar_full[kMostStages], bar_free[kMostStages], bar_acc_full[2], bar_acc_free[2], bar_end;
     __shared__ uint32_t tmem_addr;
     __shared__ int failed;
     const int warp = (int)warp_uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
-    constexpr bool kAdapters = kHeld >= 0;
     const uint32_t ring = (smem_u32(smem_raw) + 1023u) & ~1023u, staging = ring + p.ring_bytes;
     const uint32_t stage_bytes = (uint32_t)(kTileM + p.tile_n) * kBlockK;
     const int rank = p.split > 1 ? (int)(blockIdx.x % (unsigned)p.split) : 0;
@@ -519,27 +541,38 @@ template <Form kForm, int kHeld, bool kHalf> __global__ void __launch_bounds__(k
         }
         if (kAdapters && first_tile < tiles) prefetch_adapters(p, first_tile / p.tiles_m * p.tile_n, first_tile % p.tiles_m * kTileM, w, lane);
         if constexpr (kForm == kTiles) {
-            const uint32_t inner_at = staging + kEpilogueWarps * kStaging + (uint32_t)w * 2u * kInnerStage;
-            const int blocks = kAdapters ? p.ranks >> 4 : 1;
-            // sixteen rows' inner sums of sixteen ranks, brought ahead of their use (rows behind the last one: the last one's)
-            const auto fetch_inner = [&](int row0, int block, int slot) {
-                const int row = min(row0 + (lane >> 1), p.rows - 1), half_of = lane & 1;
-                const float *from = p.inner + (int64_t)row * p.ranks + 16 * block + 8 * half_of;
-                const uint32_t to = inner_at + (uint32_t)slot * kInnerStage + (uint32_t)(lane >> 1) * kInnerRow + 32u * (uint32_t)half_of;
-                conv::cp_async16(to, from);
-                conv::cp_async16(to + 16, from + 4);
-                asm volatile("cp.async.commit_group;" ::: "memory");
-            };
+            const uint32_t in_pitch = inner_pitch(p.ranks), b_pitch = left_pitch(p.ranks), inner_at = staging + kEpilogueWarps * kStaging, left_at = inner_at + (uint32_t)p.tile_n * in_pitch;
+            const uint8_t *const inner_s = smem_raw + (inner_at - smem_u32(smem_raw)), *const left_s = smem_raw + (left_at - smem_u32(smem_raw));
             if (kAdapters) conv::chain_wait();
             int j = 0;
             for (int tile = first_tile; tile < tiles; tile += tile_step, ++j) {
-                const int buf = j & 1, n0 = tile / p.tiles_m * p.tile_n;
-                strip.load(p, tile % p.tiles_m * kTileM + 32 * quarter, lane);
+                const int buf = j & 1, m0 = tile % p.tiles_m * kTileM, n0 = tile / p.tiles_m * p.tile_n;
+                strip.load(p, m0 + 32 * quarter, lane);
                 Rows<2> rows;
                 rows.load<kAdapters>(p, n0 + 16 * half, lane);
-                Left held;
-                int held_a = -1, slot = 0;
-                if (kAdapters) fetch_inner(n0 + 16 * half, 0, 0);
+                int kept = -1;
+                if (kAdapters) {
+                    // Under the tile's products: all of its rows' inner sums, and B of the adapter that its middle row has
+                    const int e = threadIdx.x - 64, words = p.ranks >> 2;
+                    kept = __ldg(p.ids + min(n0 + p.tile_n / 2, p.rows - 1));
+                    if ((unsigned)kept >= (unsigned)p.n_adapters) kept = -1;
+                    epilogue_sync();                    // the tile before has been read
+                    for (int i = e; i < p.tile_n * words; i += 32 * kEpilogueWarps) {
+                        const int row = i / words, at = i - row * words;
+                        conv::cp_async16(inner_at + (uint32_t)row * in_pitch + 16u * (uint32_t)at, p.inner + (int64_t)min(n0 + row, p.rows - 1) * p.ranks + 4 * at);
+                    }
+                    if (kept >= 0) {
+                        const uint16_t *b = static_cast<const uint16_t *>(p.b) + ((int64_t)kept * p.n + m0) * p.rank;
+                        for (int i = e; i < kTileM * words; i += 32 * kEpilogueWarps) {
+                            const int row = i / words, at = 4 * (i - row * words);
+                            const bool there = at < p.rank && m0 + row < p.n;
+                            asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;"
+                                         ::"r"(left_at + (uint32_t)row * b_pitch + 2u * (uint32_t)at), "l"(there ? b + (int64_t)row * p.rank + at : b), "r"(there ? 8 : 0) : "memory");
+                        }
+                    }
+                    conv::cp_async_wait_all();
+                    epilogue_sync();
+                }
                 const bool ok = __all_sync(0xffffffffu, wait_limited(smem_u32(&bar_acc_full[buf]), (uint32_t)(j >> 1) & 1u, &failed)) != 0;
                 if (!ok) {              // nothing of the tile can be told
                     timeout_word = 1;
@@ -561,33 +594,16 @@ template <Form kForm, int kHeld, bool kHalf> __global__ void __launch_bounds__(k
                         const int a = rows.id[0][0];
                         const int a0 = __shfl_sync(0xffffffffu, a, 0);
                         const bool same = __all_sync(0xffffffffu, (a == a0) & (a == rows.id[0][1]) & (a == rows.id[1][0]) & (a == rows.id[1][1])) != 0;
-                        if (kHeld > 0 && same && a != held_a && (unsigned)a < (unsigned)p.n_adapters) {
-                            held_a = a;
-                            held.load(p, a, strip.n0, 0, lane);
-                        }
-                        // inner sums of block r of this step's rows, once the next sixteen ranks or rows are under way
-                        const auto arrived = [&](int r) {
-                            __syncwarp();               // (the slot to be filled has been read)
-                            if (r + 1 < blocks) fetch_inner(row0, r + 1, slot ^ 1);
-                            else fetch_inner(row0 + 32, 0, slot ^ 1);
-                            asm volatile("cp.async.wait_group 1;" ::: "memory");
-                            __syncwarp();
-                            const uint8_t *from = smem_raw + (inner_at - smem_u32(smem_raw)) + (uint32_t)slot * kInnerStage + 2u * (uint32_t)(lane & 3) * kInnerRow;
-                            slot ^= 1;
-                            return [from](int e, int jj, int quad) { return *reinterpret_cast<const float4 *>(from + (uint32_t)(8 * e + jj) * kInnerRow + 16u * (uint32_t)quad); };
-                        };
-                        if (!same) {
+                        const uint8_t *from = inner_s + (uint32_t)(16 * q + 2 * (lane & 3)) * in_pitch;
 #pragma unroll 1
-                            for (int r = 0; r < blocks; ++r) add_each<kHalf, 2>(p, rows, strip.n0, r, lane, arrived(r), outer);
-                        } else if (kHeld > 0) {
-                            const auto inner = arrived(0);
-                            if ((unsigned)a < (unsigned)p.n_adapters) outer.template add<kHalf, -1>(held, inner);
-                        } else {
-#pragma unroll 1
-                            for (int r = 0; r < blocks; ++r) {
-                                if ((unsigned)a < (unsigned)p.n_adapters) held.load(p, a, strip.n0, r, lane);
-                                const auto inner = arrived(r);
-                                if ((unsigned)a < (unsigned)p.n_adapters) outer.template add<kHalf, -1>(held, inner);
+                        for (int r = 0; r < p.ranks >> 4; ++r, from += 64) {
+                            const auto inner = [&](int e, int jj, int quad) { return *reinterpret_cast<const float4 *>(from + (uint32_t)(8 * e + jj) * in_pitch + 16u * (uint32_t)quad); };
+                            if (!same) add_each<kHalf, 2>(p, rows, strip.n0, r, lane, inner, outer);
+                            else if ((unsigned)a < (unsigned)p.n_adapters) {
+                                Left left;
+                                if (a == kept) load_kept(left, left_s + (uint32_t)(32 * quarter) * b_pitch, b_pitch, r, lane);
+                                else left.load(p, a, strip.n0, r, lane);
+                                outer.template add<kHalf, -1>(left, inner);
                             }
                         }
                     }
@@ -600,7 +616,6 @@ template <Form kForm, int kHeld, bool kHalf> __global__ void __launch_bounds__(k
                     }
                     rows = next;
                 }
-                if (kAdapters) asm volatile("cp.async.wait_all;" ::: "memory");
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(smem_u32(&bar_acc_free[buf]));
@@ -921,7 +936,7 @@ bool encode_rows(void *encode, CUtensorMap *map, const int8_t *base, int64_t k, 
 void plan(LinearParams &p, int n_sms)
 {
     p.tiles_m = (p.n + kTileM - 1) / kTileM;
-    const int least = (p.rows + kMostTileN - 1) / kMostTileN;
+    const int most = widest_tile(p.ranks), widest = p.rows <= 1024 ? kMostTileN : most, least = (p.rows + widest - 1) / widest;
     int64_t best = INT64_MAX;
     for (int t = least; t <= std::min(4 * least + 4, least + 64); ++t) {
         const int width = ((p.rows + t - 1) / t + 15) & ~15, tiles_n = (p.rows + width - 1) / width;
@@ -931,8 +946,9 @@ void plan(LinearParams &p, int n_sms)
         const int64_t tiles = (int64_t)p.tiles_m * tiles_n, slots = narrow ? 2 * n_sms : n_sms;
         for (int split = 1; split <= kMostSplit && (split == 1 || (tiles * split <= slots && p.k_blocks >= 4 * split)); split *= 2) {
             const bool part = narrow || split > 1;
+            if (!part && width > most) continue;
             const int64_t rounds = (tiles * split + slots - 1) / slots;
-            const double products = 2.1 * ((p.k_blocks + split - 1) / split) * (width + kTileM), end = (25.0 + 50.0 * (p.ranks >> 4)) * width / split + (split > 1 ? 2000.0 : 0.0);
+            const double products = 2.1 * ((p.k_blocks + split - 1) / split) * (width + kTileM), end = (25.0 + (part ? 50.0 : 25.0) * (p.ranks >> 4)) * width / split + (split > 1 ? 2000.0 : 0.0);
             const int64_t cost = (int64_t)(part ? rounds * (products + end + 3000.0) : rounds * std::max(products, end) + std::min(products, end) + 3000.0);
             if (cost < best) {
                 best = cost;
@@ -940,7 +956,7 @@ void plan(LinearParams &p, int n_sms)
                 p.tiles_n = tiles_n;
                 p.split = split;
                 p.form = part ? kPart : kTiles;
-                p.ring_bytes = narrow ? kRingBytesNarrow : kRingBytes;
+                p.ring_bytes = narrow ? kRingBytesNarrow : part ? kRingBytes : (uint32_t)(4 * (kTileM + most) * kBlockK);
             }
         }
     }
@@ -1052,13 +1068,12 @@ extern "C" int isc_quant_linear(const int8_t *x, int64_t ldx, const float *x_sca
     if ((int64_t)p.tiles_m * p.tiles_n > INT32_MAX / kMostSplit) return ISC_ERR_UNSUPPORTED;
     if (!dev.encode || !encode_rows(dev.encode, &p.map_w, w, k, n, ldw, kTileM) || !encode_rows(dev.encode, &p.map_x, x, k, rows, ldx, p.tile_n)) return ISC_ERR_CUDA;
     void (*const kernel)(LinearParams) =
-        p.form == kPart ? (!ad ? k_quant_linear<kPart, -1, false> : half ? k_quant_linear<kPart, 0, true> : k_quant_linear<kPart, 0, false>) :
-        !ad ? k_quant_linear<kTiles, -1, false> :
-        ad->rank <= 16 ? (half ? k_quant_linear<kTiles, 1, true> : k_quant_linear<kTiles, 1, false>) : half ? k_quant_linear<kTiles, 0, true> : k_quant_linear<kTiles, 0, false>;
-    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(kRingBytes + kSmemTiles));
+        p.form == kPart ? (!ad ? k_quant_linear<kPart, false, false> : half ? k_quant_linear<kPart, true, true> : k_quant_linear<kPart, true, false>) :
+        !ad ? k_quant_linear<kTiles, false, false> : half ? k_quant_linear<kTiles, true, true> : k_quant_linear<kTiles, true, false>;
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemMost);
     if (e != cudaSuccess) return status_of(e, "quant_linear");
     const int tiles = p.tiles_m * p.tiles_n;
     const unsigned grid = p.form == kPart ? (unsigned)(tiles * p.split) : (unsigned)std::min(tiles, dev.n_sms);
-    e = launch(kernel, p, dim3(grid), kThreads, p.ring_bytes + (p.form == kPart ? kSmemPart : kSmemTiles), p.split, ad != nullptr, st);
+    e = launch(kernel, p, dim3(grid), kThreads, p.ring_bytes + kSmemBeside + (p.form == kTiles && ad ? p.tile_n * inner_pitch(p.ranks) + kTileM * left_pitch(p.ranks) : 0), p.split, ad != nullptr, st);
     return status_of(e, "quant_linear");
 }
