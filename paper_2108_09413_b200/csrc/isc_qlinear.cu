@@ -52,11 +52,12 @@ constexpr size_t kSmemMost = 231936;
 // eight outputs that a warp reads at once lie in different banks.
 __host__ __device__ constexpr uint32_t inner_pitch(int ranks) { return (uint32_t)ranks * 4u + 16u; }
 __host__ __device__ constexpr uint32_t left_pitch(int ranks) { return (uint32_t)ranks * 2u + 8u; }
-// the widest tile that leaves them room beside four stages
+constexpr size_t adapter_bytes(int ranks, int width) { return ranks ? width * inner_pitch(ranks) + kTileM * left_pitch(ranks) : 0; }
+// the widest tile that leaves them room beside three stages
 constexpr int widest_tile(int ranks)
 {
     int width = kMostTileN;
-    while (width > 16 && (size_t)(4 * (kTileM + width) * kBlockK) + kSmemBeside + (ranks ? width * inner_pitch(ranks) + kTileM * left_pitch(ranks) : 0) > kSmemMost) width -= 16;
+    while (width > 16 && (size_t)(3 * (kTileM + width) * kBlockK) + kSmemBeside + adapter_bytes(ranks, width) > kSmemMost) width -= 16;
     return width;
 }
 
@@ -956,7 +957,7 @@ void plan(LinearParams &p, int n_sms)
                 p.tiles_n = tiles_n;
                 p.split = split;
                 p.form = part ? kPart : kTiles;
-                p.ring_bytes = narrow ? kRingBytesNarrow : part ? kRingBytes : (uint32_t)(4 * (kTileM + most) * kBlockK);
+                p.ring_bytes = narrow ? kRingBytesNarrow : part ? kRingBytes : (uint32_t)(kSmemMost - kSmemBeside - adapter_bytes(p.ranks, width)) & ~1023u;
             }
         }
     }
@@ -1074,6 +1075,6 @@ extern "C" int isc_quant_linear(const int8_t *x, int64_t ldx, const float *x_sca
     if (e != cudaSuccess) return status_of(e, "quant_linear");
     const int tiles = p.tiles_m * p.tiles_n;
     const unsigned grid = p.form == kPart ? (unsigned)(tiles * p.split) : (unsigned)std::min(tiles, dev.n_sms);
-    e = launch(kernel, p, dim3(grid), kThreads, p.ring_bytes + kSmemBeside + (p.form == kTiles && ad ? p.tile_n * inner_pitch(p.ranks) + kTileM * left_pitch(p.ranks) : 0), p.split, ad != nullptr, st);
+    e = launch(kernel, p, dim3(grid), kThreads, p.ring_bytes + kSmemBeside + (p.form == kTiles ? adapter_bytes(p.ranks, p.tile_n) : 0), p.split, ad != nullptr, st);
     return status_of(e, "quant_linear");
 }
