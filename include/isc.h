@@ -440,8 +440,8 @@ int isc_quant_linear_work_space(int64_t rows, int rank, int64_t *out_bytes);
  *   out_top_ids, out_top_log_probs : [rows][top]  the `top` tokens of the largest logits in falling order, ties to the
  *                   lowest index, and their log probabilities.
  *   votes         : [vocab] int32; 1 is added to the entry of each row's first token.
- *   logits : [rows][vocab] of `type`, any isc_type.   targets : [rows] int64.   0 <= top <= 32.   scale > 0 (the inverse
- *   temperature).  Any of targets (with out_log_probs), out_entropy, votes may be NULL, out_top_* only with top = 0.
+ *   logits : [rows][vocab] of `type`, any isc_type.   targets : [rows] int64.   0 <= top <= 32.   0 < scale <= 1e38 (the
+ *   inverse temperature).  Any of targets (with out_log_probs), out_entropy, votes may be NULL, out_top_* only with top = 0.
  * A logit of minus infinity is masked: probability 0, never an alternative.  Where a row has fewer than `top` others, the
  * rest of its alternatives has id -1 and log probability -inf.  A row with nothing but masks has log probability -inf,
  * entropy 0 and no vote.  A row with a NaN or plus infinity has NaN results, ids -1 and no vote.

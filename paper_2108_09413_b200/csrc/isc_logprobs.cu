@@ -777,7 +777,7 @@ extern "C" int isc_log_probs(const void *logits, int64_t ld, int type, int64_t r
 {
     using namespace isc;
     using namespace isc::ops;
-    if (rows < 0 || vocab < 1 || (!is_float_type(type) && type != ISC_I8) || !(scale > 0.0f) || scale > FLT_MAX || top < 0 || top > kMostTop) return ISC_ERR_ARG;
+    if (rows < 0 || vocab < 1 || (!is_float_type(type) && type != ISC_I8) || !(scale > 0.0f) || scale > 1e38f || top < 0 || top > kMostTop) return ISC_ERR_ARG;
     if (rows == 0) return ISC_OK;
     if (!logits || ld < vocab || (targets != nullptr) != (out_log_probs != nullptr) || (top > 0 && (!out_top_ids || !out_top_log_probs))) return ISC_ERR_ARG;
     if (!aligned(logits, type_bytes(type)) || !aligned(targets, 8) || !aligned(out_log_probs, 4) || !aligned(out_entropy, 4) || !aligned(out_top_ids, 4) || !aligned(out_top_log_probs, 4) ||

@@ -37,7 +37,7 @@ LOGS_GOOD = [AT, 100, 0, 4, 100, 1.0, AT, 5, AT, AT, AT, AT, AT, None]
 
 @pytest.mark.parametrize("what,value,expected", [
     ("logits", None, ARG), ("logits", AT + 1, ARG), ("ld", 99, ARG), ("ld", 0, ARG), ("type", 4, ARG), ("type", -1, ARG), ("rows", -1, ARG), ("vocab", 0, ARG),
-    ("scale", 0.0, ARG), ("scale", -1.0, ARG), ("scale", float("nan"), ARG), ("scale", float("inf"), ARG), ("targets", None, ARG), ("log_probs", None, ARG),
+    ("scale", 0.0, ARG), ("scale", -1.0, ARG), ("scale", float("nan"), ARG), ("scale", float("inf"), ARG), ("scale", 2e38, ARG), ("targets", None, ARG), ("log_probs", None, ARG),
     ("targets", AT + 4, ARG), ("entropy", AT + 2, ARG), ("votes", AT + 1, ARG), ("top_ids", None, ARG), ("top_log_probs", None, ARG), ("top", 33, ARG), ("top", -1, ARG),
     ("rows", 2**31, UNSUPPORTED), ("vocab", 2**31, UNSUPPORTED), ("rows", 0, OK)])
 def test_log_probs(what, value, expected):
