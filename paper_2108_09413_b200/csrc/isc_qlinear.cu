@@ -43,10 +43,11 @@ __device__ int timeout_word;            // not zero: a bounded wait has run out
 constexpr int kTileM = 128, kBlockK = 128;
 constexpr int kEpilogueWarps = 8, kThreads = 32 * (2 + kEpilogueWarps);
 constexpr int kMostStages = 12, kMostTileN = 256, kMostSplit = 8;
-constexpr uint32_t kRingBytes = 192 * 1024, kRingBytesNarrow = 96 * 1024;
+constexpr uint32_t kRingBytes = 192 * 1024, kRingBytesNarrow = 72 * 1024;
 constexpr uint32_t kStageRow = 80, kStageRowWide = 144;      // bytes from row to row of a warp's output staging (16-bit, 32-bit)
 constexpr uint32_t kStaging = 8 * kStageRowWide;
 constexpr size_t kSmemBeside = kEpilogueWarps * kStaging + 1024;       // beside the stages
+constexpr int kOuterAhead = 4;          // of a warp's items, whose outer products are computed ahead (kPart)
 constexpr size_t kSmemMost = 231936;
 // A tile's inner sums, and its adapter's B, in shared memory: bytes from row to row and from output to output, so that the four rows and the
 // eight outputs that a warp reads at once lie in different banks.
@@ -392,47 +393,56 @@ template <int kSplit> __device__ __forceinline__ void gather(uint32_t at, int (&
     }
 }
 
-// 32 outputs x 8 rows of a tile whose sums lie in the shared memory of the blocks that share it ([output][row], at `sums`).
-template <bool kAdapters, bool kHalf, int kLanes> __device__ __forceinline__ void finish_part(const LinearParams &p, int row0, int n0, uint32_t sums, int lane, bool failed)
+// The outer products of 32 outputs x 8 rows, each row with its own adapter, to shared memory ([row][output], single precision).
+template <bool kHalf, int kLanes> __device__ __forceinline__ void outer_rows_by(const LinearParams &p, int row0, int n0, int lane, uint32_t to)
 {
-    const int out = output_of<kLanes>(lane), n = n0 + out, mine = row0 + (lane & 7);
-    const float w_scale = n < p.n ? __ldg(p.w_scale + n) : 0.0f, bias = p.bias && n < p.n ? __ldg(p.bias + n) : 0.0f, x_scale = mine < p.rows ? __ldg(p.x_scale + mine) : 0.0f;
-    const int id = kAdapters && mine < p.rows ? __ldg(p.ids + mine) : -1;
+    const int mine = row0 + (lane & 7), id = mine < p.rows ? __ldg(p.ids + mine) : -1;
     constexpr int kTogether = kLanes < 8 ? 8 / kLanes : 1;       // rows whose operands are loaded together
-    int sums8[8] = {};
-    const uint32_t from = sums + (uint32_t)out * 32u;
-    if (p.split == 1) gather<1>(from, sums8);
-    else if (p.split == 2) gather<2>(from, sums8);
-    else if (p.split == 4) gather<4>(from, sums8);
-    else { gather<4>(from, sums8); gather<4>(from, sums8, 4); }
 #pragma unroll 1
     for (int t0 = 0; t0 < 8; t0 += kTogether) {
-        if (row0 + t0 >= p.rows) break;
         float outer[kTogether];
-        int sum[kTogether], a[kTogether];
 #pragma unroll
         for (int u = 0; u < kTogether; ++u) {
-            a[u] = __shfl_sync(0xffffffffu, id, t0 + u);
-            sum[u] = sums8[u];
-#pragma unroll
-            for (int t = 1; t < 8; ++t)
-                if (t == t0 + u) sum[u] = sums8[t];          // (registers have no index)
+            const int a = __shfl_sync(0xffffffffu, id, t0 + u);
+            outer[u] = (unsigned)a < (unsigned)p.n_adapters ? outer_of<kHalf, kLanes>(p, a, row0 + t0 + u, n0, lane) : 0.0f;
         }
 #pragma unroll
-        for (int u = 0; u < kTogether; ++u) {
-            outer[u] = 0.0f;
-            if (kAdapters && (unsigned)a[u] < (unsigned)p.n_adapters) outer[u] = outer_of<kHalf, kLanes>(p, a[u], row0 + t0 + u, n0, lane);
-        }
+        for (int u = 0; u < kTogether; ++u)
+            asm volatile("st.shared.f32 [%0], %1;" ::"r"(to + (uint32_t)((t0 + u) * 32 + output_of<kLanes>(lane)) * 4u), "f"(outer[u]) : "memory");
+    }
+    __syncwarp();
+}
+template <bool kHalf> __device__ __forceinline__ void outer_rows(const LinearParams &p, int row0, int n0, int lane, uint32_t to)
+{
+    if (p.rank <= 16) outer_rows_by<kHalf, 2>(p, row0, n0, lane, to);
+    else if (p.rank <= 32) outer_rows_by<kHalf, 4>(p, row0, n0, lane, to);
+    else if (p.rank <= 64) outer_rows_by<kHalf, 8>(p, row0, n0, lane, to);
+    else outer_rows_by<kHalf, 16>(p, row0, n0, lane, to);
+}
+
+// 32 outputs x 8 rows of a tile whose sums lie in the shared memory of the blocks that share it ([output][row], at `sums`); `outer`: where
+// outer_rows has put theirs.  A lane has an output.
+template <bool kAdapters> __device__ __forceinline__ void finish_part(const LinearParams &p, int row0, int n0, uint32_t sums, uint32_t outer, int lane, bool failed)
+{
+    const int n = n0 + lane, mine = row0 + (lane & 7);
+    const float w_scale = n < p.n ? __ldg(p.w_scale + n) : 0.0f, bias = p.bias && n < p.n ? __ldg(p.bias + n) : 0.0f;
+    const int id = kAdapters && mine < p.rows ? __ldg(p.ids + mine) : -1;
+    const float x_scale = failed || (kAdapters && id >= p.n_adapters) ? NAN : mine < p.rows ? __ldg(p.x_scale + mine) : 0.0f;
+    int sum[8] = {};
+    const uint32_t from = sums + (uint32_t)lane * 32u;
+    if (p.split == 1) gather<1>(from, sum);
+    else if (p.split == 2) gather<2>(from, sum);
+    else if (p.split == 4) gather<4>(from, sum);
+    else { gather<4>(from, sum); gather<4>(from, sum, 4); }
 #pragma unroll
-        for (int u = 0; u < kTogether; ++u) {
-            const float scale = __shfl_sync(0xffffffffu, x_scale, t0 + u);
-            const float f = failed || (kAdapters && a[u] >= p.n_adapters) ? NAN : fmaf(fmaf(w_scale, (float)sum[u], outer[u]), scale, bias);
-            if (row0 + t0 + u >= p.rows || n >= p.n) continue;
-            const int64_t at = (int64_t)(row0 + t0 + u) * p.ldy + n;
-            if (p.y_type == ISC_F32) static_cast<float *>(p.y)[at] = f;
-            else if (p.y_type == ISC_F16) static_cast<__half *>(p.y)[at] = __float2half_rn(f);
-            else static_cast<__nv_bfloat16 *>(p.y)[at] = __float2bfloat16_rn(f);
-        }
+    for (int t = 0; t < 8; ++t) {
+        const float part = kAdapters ? __uint_as_float(lds32(outer + (uint32_t)(t * 32 + lane) * 4u)) : 0.0f;
+        const float f = fmaf(fmaf(w_scale, (float)sum[t], part), __shfl_sync(0xffffffffu, x_scale, t), bias);
+        if (row0 + t >= p.rows || n >= p.n) continue;
+        const int64_t at = (int64_t)(row0 + t) * p.ldy + n;
+        if (p.y_type == ISC_F32) static_cast<float *>(p.y)[at] = f;
+        else if (p.y_type == ISC_F16) static_cast<__half *>(p.y)[at] = __float2half_rn(f);
+        else static_cast<__nv_bfloat16 *>(p.y)[at] = __float2bfloat16_rn(f);
     }
 }
 
@@ -461,7 +471,7 @@ template <Form kForm, bool kAdapters, bool kHalf> __global__ void __launch_bound
     __shared__ uint32_t tmem_addr;
     __shared__ int failed;
     const int warp = (int)warp_uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
-    const uint32_t ring = (smem_u32(smem_raw) + 1023u) & ~1023u, staging = ring + p.ring_bytes;
+    const uint32_t ring = (smem_u32(smem_raw) + 1023u) & ~1023u, staging = ring + p.ring_bytes, outer_at = staging;     // (kPart has no other use for it)
     const uint32_t stage_bytes = (uint32_t)(kTileM + p.tile_n) * kBlockK;
     const int rank = p.split > 1 ? (int)(blockIdx.x % (unsigned)p.split) : 0;
     const int first_tile = (int)(blockIdx.x / (unsigned)p.split), tile_step = (int)(gridDim.x / (unsigned)p.split), tiles = p.tiles_m * p.tiles_n;
@@ -626,6 +636,14 @@ template <Form kForm, bool kAdapters, bool kHalf> __global__ void __launch_bound
                 if (lane == 0) mbar_arrive(smem_u32(&bar_acc_free[buf]));
             }
         } else {
+            if (kAdapters) {
+                // the first items' outer products, under W's copies and products: they need the inner sums only
+                conv::chain_wait();
+                for (int i = 0; i < kOuterAhead; ++i) {
+                    const int item = rank + p.split * (w + kEpilogueWarps * i), row0 = first_tile / p.tiles_m * p.tile_n + item % (p.tile_n / 8) * 8, strip_n = first_tile % p.tiles_m * kTileM + 32 * (item / (p.tile_n / 8));
+                    if (item < kTileM / 32 * (p.tile_n / 8) && row0 < p.rows && strip_n < p.n) outer_rows<kHalf>(p, row0, strip_n, lane, outer_at + (uint32_t)(w * kOuterAhead + i) * 1024u);
+                }
+            }
             // this block's sums to its shared memory; its ring is empty: all products are done
             const bool ok = __all_sync(0xffffffffu, wait_limited(smem_u32(&bar_acc_full[0]), 0, &failed)) != 0;
             if (!ok) timeout_word = 1;
@@ -652,15 +670,13 @@ template <Form kForm, bool kAdapters, bool kHalf> __global__ void __launch_bound
             const int w = warp - 2, per_quarter = p.tile_n / 8;
             bool bad = false;
             for (int b = 0; b < p.split; ++b) bad |= read_remote(in_block(smem_u32(&failed), b)) != 0;
-            if (kAdapters) conv::chain_wait();
-            for (int item = rank + p.split * w; item < kTileM / 32 * per_quarter; item += p.split * kEpilogueWarps) {
+            int i = 0;
+            for (int item = rank + p.split * w; item < kTileM / 32 * per_quarter; item += p.split * kEpilogueWarps, ++i) {
                 const int at = item % per_quarter * 8, row0 = first_tile / p.tiles_m * p.tile_n + at, strip = item / per_quarter, n0 = first_tile % p.tiles_m * kTileM + 32 * strip;
                 if (row0 >= p.rows || n0 >= p.n) continue;
-                const uint32_t sums = ring + (uint32_t)item * 1024u;
-                if (!kAdapters || p.rank <= 16) finish_part<kAdapters, kHalf, 2>(p, row0, n0, sums, lane, bad);
-                else if (p.rank <= 32) finish_part<kAdapters, kHalf, 4>(p, row0, n0, sums, lane, bad);
-                else if (p.rank <= 64) finish_part<kAdapters, kHalf, 8>(p, row0, n0, sums, lane, bad);
-                else finish_part<kAdapters, kHalf, 16>(p, row0, n0, sums, lane, bad);
+                const uint32_t outer = outer_at + (uint32_t)(w * kOuterAhead + i % kOuterAhead) * 1024u;
+                if (kAdapters && i >= kOuterAhead) outer_rows<kHalf>(p, row0, n0, lane, outer);
+                finish_part<kAdapters>(p, row0, n0, ring + (uint32_t)item * 1024u, outer, lane, bad);
             }
         }
         __syncwarp();
@@ -964,7 +980,7 @@ void plan(LinearParams &p, int n_sms)
                 p.tiles_n = tiles_n;
                 p.split = split;
                 p.form = part ? kPart : kTiles;
-                p.ring_bytes = narrow ? kRingBytesNarrow : part ? kRingBytes : (uint32_t)(kSmemMost - kSmemBeside - adapter_bytes(p.ranks, width)) & ~1023u;
+                p.ring_bytes = narrow ? (p.ranks ? kRingBytesNarrow : kRingBytesNarrow + 24 * 1024) : part ? kRingBytes : (uint32_t)(kSmemMost - kSmemBeside - adapter_bytes(p.ranks, width)) & ~1023u;
             }
         }
     }
@@ -1084,6 +1100,6 @@ extern "C" int isc_quant_linear(const int8_t *x, int64_t ldx, const float *x_sca
     if (e != cudaSuccess) return status_of(e, "quant_linear");
     const int tiles = p.tiles_m * p.tiles_n;
     const unsigned grid = p.form == kPart ? (unsigned)(tiles * p.split) : (unsigned)std::min(tiles, dev.n_sms);
-    e = launch(kernel, p, dim3(grid), kThreads, p.ring_bytes + kSmemBeside + (p.form == kTiles ? adapter_bytes(p.ranks, p.tile_n) : 0), p.split, ad != nullptr, st);
+    e = launch(kernel, p, dim3(grid), kThreads, p.ring_bytes + kSmemBeside + (p.form == kTiles ? adapter_bytes(p.ranks, p.tile_n) : ad ? kEpilogueWarps * (kOuterAhead * 1024 - kStaging) : 0), p.split, ad != nullptr, st);
     return status_of(e, "quant_linear");
 }
