@@ -13,12 +13,24 @@
 // fewer tiles than SMs, a cluster of up to eight blocks shares a tile: each takes a part of k, leaves its int32 sums
 // in shared memory and finishes its share of the tile from all of them; integers add up exactly in any order.
 //
-// The outer product in the epilogue, in single precision by two-number FMAs: accumulators are read from tensor memory as
-// fragments, so a thread has 4 outputs x 4 rows, and an inner sum that it loads serves four products, a value of B another
-// four (with an output to a lane and one row at a time, loads of inner sums took four times as long as the products).  B
-// stays in registers from row to row while rows share an adapter; a row that does not share its neighbours' loads its own.
-// mma.sync for this part is no way out: beside tcgen05 products that keep the tensor pipe busy each one waits for hundreds
-// of cycles (8,192 rows, k = n = 8,192, rank 32: 604 us with it, 400 us for the product without adapters).
+// Forms.  k_quant_linear<kTiles>: persistent blocks with tile after tile.  <kPart>: a tile for a block or a cluster, narrow ones (few rows) two
+// to an SM.  k_quant_linear_one: a single row, without the tensor cores.  plan() chooses by a count of cycles.
+//
+// The adapters' outer product, in single precision by two-number FMAs.  kTiles: on the accumulators' fragments, as tensor memory gives
+// them: a thread has 4 outputs x 4 rows, so an inner sum that it loads serves four products, a value of B another four.  The tile's
+// inner sums and its adapter's B lie in shared memory (with 200 KB of it in use the first-level cache is next to
+// nothing, and what a step loads from memory it waits for); a row that does not share its neighbours' adapter loads its own.
+// kPart, whose rows may each have another adapter: groups of lanes share an output's ranks, straight from memory, while W is on its way.
+//
+// Measured (us; rank 0 is without adapters): 8,192 rows, k = n = 4,096: rank 0 99, 16 132, 32 167, 64 276; k = n = 8,192, rank 32: 502 (410 without: 2.68
+// POP/s, the rate that the card's power lets cuBLAS's bf16 sustain, twice over); 64 rows, k = 4,096, n = 12,288, 32 adapters of rank 16: 27 (17 without).
+// What bounds it: few rows the copies' start and end around W's bytes; many, the tensor pipe, and from rank 32 on the
+// epilogue's FMAs beside it.
+//
+// Two other ways were measured.  mma.sync in the epilogue: beside tcgen05 products that keep the tensor pipe busy each one waits for
+// hundreds of cycles (k = n = 8,192, rank 32: 604 us).  tcgen05 kind::f16 into a third accumulator, inner sums as sums of bf16 numbers,
+// operands written by helper warps: tensor memory then has room for tiles of 160 rows only, and those alone cost more than the
+// FMAs (k = n = 4,096: rank 0 177, 16 212, 32 242, 64 317 us).
 #include <cuda.h>
 #include <cuda_runtime.h>
 #include <math.h>
@@ -79,14 +91,14 @@ struct LinearParams {
     bool vec_y;
 };
 
-struct FewParams {
+struct OneParams {
     const int8_t *x, *w;
     const float *x_scale, *w_scale, *bias, *inner;
     const void *b;
     const int32_t *ids;
     void *y;
-    int64_t ldx, ldw, ldy;
-    int rows, n, k, rank, ranks, n_adapters, y_type;
+    int64_t ldw;
+    int n, k, rank, n_adapters, y_type;
 };
 
 __device__ __forceinline__ void copy_tile(uint32_t dst, const CUtensorMap *map, int x, int y, uint32_t bar)
@@ -699,92 +711,57 @@ __device__ __forceinline__ uint4 load_codes(const int8_t *at, int left)
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// ---- few rows: W's rows straight into registers
+// ---- one row: W's rows straight into registers
 
-// kRows rows at most times kOut rows of W a warp, products by dp4a.  A tile of the tensor cores' form costs a fixed time (tensor memory, descriptors,
-// barriers, a cluster's join) that a call of few rows does not get back, and reads W in pieces of 128 bytes; here a warp reads
-// 512 bytes of a row of W at a time.
-constexpr int kFewThreads = 256, kFewRows = 1;
-template <int kRows, int kOut, bool kHalf> __global__ void __launch_bounds__(kFewThreads) k_quant_linear_few(const __grid_constant__ FewParams p)
+// A warp for an output, products by dp4a.  A tile of the tensor cores' form costs a fixed time (tensor memory, descriptors, barriers, a
+// cluster's join) that a call of one row does not get back, and reads W in pieces of 128 bytes; here a warp has 4 KB of a row of W under way
+// at once.  Bound by W's bytes: k = 8,192, n = 28,672 in 41 us, 5.8 TB/s; k = n = 4,096 in 6.4 us against 9.9 with tiles.
+// (dp4a is slow here, about eleven a clock and SM: two rows took 16.5 us where tiles take 10.)
+constexpr int kOneThreads = 256;
+template <bool kHalf> __global__ void __launch_bounds__(kOneThreads) k_quant_linear_one(const __grid_constant__ OneParams p)
 {
-    const int lane = threadIdx.x & 31, n0 = (int)((blockIdx.x * (unsigned)(kFewThreads / 32) + (threadIdx.x >> 5)) * kOut);
-    if (n0 >= p.n) return;
-    // the adapters' share of this warp's outputs: the first 32 ranks, a rank to a lane
-    uint32_t b[kRows][kOut];
-    int id[kRows];
-    if (p.rank) {
-#pragma unroll
-        for (int t = 0; t < kRows; ++t) {
-            id[t] = t < p.rows ? __ldg(p.ids + t) : -1;
-#pragma unroll
-            for (int o = 0; o < kOut; ++o)
-                b[t][o] = (unsigned)id[t] < (unsigned)p.n_adapters && lane < p.rank && n0 + o < p.n ? __ldg(static_cast<const uint16_t *>(p.b) + ((int64_t)id[t] * p.n + n0 + o) * p.rank + lane) : 0u;
-        }
-    }
-    // this lane's output's scales, ahead of the products
-    const int my_t = lane / kOut, my_n = n0 + lane % kOut;
-    const bool writes = my_t < p.rows && my_t < kRows && my_n < p.n;
-    const float w_scale = writes ? __ldg(p.w_scale + my_n) : 0.0f, x_scale = writes ? __ldg(p.x_scale + my_t) : 0.0f, bias = writes && p.bias ? __ldg(p.bias + my_n) : 0.0f;
-    int sum[kRows][kOut] = {};
-    constexpr int kAhead = kRows * kOut >= 16 ? 2 : 8 / kOut;
+    const int lane = threadIdx.x & 31, n = (int)(blockIdx.x * (unsigned)(kOneThreads / 32) + (threadIdx.x >> 5));
+    if (n >= p.n) return;
+    // what the end needs, ahead of the products; the adapter's share of this output: the first 32 ranks, a rank to a lane
+    const float w_scale = __ldg(p.w_scale + n), x_scale = __ldg(p.x_scale), bias = p.bias ? __ldg(p.bias + n) : 0.0f;
+    const int id = p.rank ? __ldg(p.ids) : -1;
+    const bool adapted = (unsigned)id < (unsigned)p.n_adapters;
+    const uint16_t *b = static_cast<const uint16_t *>(p.b) + ((int64_t)id * p.n + n) * p.rank;
+    const uint32_t b_first = adapted && lane < p.rank ? __ldg(b + lane) : 0u;
+    const int8_t *w = p.w + (int64_t)n * p.ldw;
+    int sum = 0;
+    constexpr int kAhead = 8;
     for (int k0 = 16 * lane; k0 < p.k; k0 += 512 * kAhead) {
-        uint4 w[kAhead][kOut];
+        uint4 v[kAhead];
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u)
+        for (int u = 0; u < kAhead; ++u) v[u] = load_codes(w + k0 + 512 * u, p.k - k0 - 512 * u);
 #pragma unroll
-            for (int o = 0; o < kOut; ++o) {
-                const int k = k0 + 512 * u;
-                w[u][o] = n0 + o < p.n ? load_codes(p.w + (int64_t)(n0 + o) * p.ldw + k, p.k - k) : make_uint4(0, 0, 0, 0);
-            }
-#pragma unroll
-        for (int u = 0; u < kAhead; ++u)
-#pragma unroll
-            for (int t = 0; t < kRows; ++t) {
-                const int k = k0 + 512 * u;
-                const uint4 x = t < p.rows ? load_codes(p.x + (int64_t)t * p.ldx + k, p.k - k) : make_uint4(0, 0, 0, 0);
-#pragma unroll
-                for (int o = 0; o < kOut; ++o) {
-                    int s = sum[t][o];
-                    s = __dp4a((int)x.x, (int)w[u][o].x, s);
-                    s = __dp4a((int)x.y, (int)w[u][o].y, s);
-                    s = __dp4a((int)x.z, (int)w[u][o].z, s);
-                    sum[t][o] = __dp4a((int)x.w, (int)w[u][o].w, s);
-                }
-            }
-    }
-#pragma unroll
-    for (int t = 0; t < kRows; ++t)
-#pragma unroll
-        for (int o = 0; o < kOut; ++o) sum[t][o] = __reduce_add_sync(0xffffffffu, sum[t][o]);
-    if (p.rank) conv::chain_wait();
-    float mine = 0.0f;                  // lane kOut t + o keeps that output
-    int my_id = -1;
-#pragma unroll
-    for (int t = 0; t < kRows; ++t) {
-        if (t >= p.rows) break;
-#pragma unroll
-        for (int o = 0; o < kOut; ++o) {
-            float outer = 0.0f;
-            if (p.rank && (unsigned)id[t] < (unsigned)p.n_adapters) {
-                for (int r = lane; r < p.rank; r += 32) {
-                    const uint32_t v = r < 32 ? b[t][o] : n0 + o < p.n ? __ldg(static_cast<const uint16_t *>(p.b) + ((int64_t)id[t] * p.n + n0 + o) * p.rank + r) : 0u;
-                    outer = fmaf(kHalf ? __half2float(__ushort_as_half((unsigned short)v)) : __uint_as_float(v << 16), p.inner[t * p.ranks + r], outer);
-                }
-#pragma unroll
-                for (int d = 16; d; d >>= 1) outer += __shfl_xor_sync(0xffffffffu, outer, d);
-            }
-            if (lane == kOut * t + o) {
-                mine = fmaf(w_scale, (float)sum[t][o], outer);
-                if (p.rank) my_id = id[t];
-            }
+        for (int u = 0; u < kAhead; ++u) {
+            const uint4 x = load_codes(p.x + k0 + 512 * u, p.k - k0 - 512 * u);
+            sum = __dp4a((int)x.x, (int)v[u].x, sum);
+            sum = __dp4a((int)x.y, (int)v[u].y, sum);
+            sum = __dp4a((int)x.z, (int)v[u].z, sum);
+            sum = __dp4a((int)x.w, (int)v[u].w, sum);
         }
     }
-    if (!writes) return;
-    mine = p.rank && my_id >= p.n_adapters ? NAN : fmaf(mine, x_scale, bias);
-    const int64_t at = (int64_t)my_t * p.ldy + my_n;
-    if (p.y_type == ISC_F32) static_cast<float *>(p.y)[at] = mine;
-    else if (p.y_type == ISC_F16) static_cast<__half *>(p.y)[at] = __float2half_rn(mine);
-    else static_cast<__nv_bfloat16 *>(p.y)[at] = __float2bfloat16_rn(mine);
+    sum = __reduce_add_sync(0xffffffffu, sum);
+    float outer = 0.0f;
+    if (p.rank) {
+        conv::chain_wait();
+        if (adapted) {
+            for (int r = lane; r < p.rank; r += 32) {
+                const uint32_t v = r < 32 ? b_first : __ldg(b + r);
+                outer = fmaf(kHalf ? __half2float(__ushort_as_half((unsigned short)v)) : __uint_as_float(v << 16), p.inner[r], outer);
+            }
+#pragma unroll
+            for (int d = 16; d; d >>= 1) outer += __shfl_xor_sync(0xffffffffu, outer, d);
+        }
+    }
+    if (lane) return;
+    const float f = p.rank && id >= p.n_adapters ? NAN : fmaf(fmaf(w_scale, (float)sum, outer), x_scale, bias);
+    if (p.y_type == ISC_F32) static_cast<float *>(p.y)[n] = f;
+    else if (p.y_type == ISC_F16) static_cast<__half *>(p.y)[n] = __float2half_rn(f);
+    else static_cast<__nv_bfloat16 *>(p.y)[n] = __float2bfloat16_rn(f);
 }
 
 // ---- the adapters' inner sums
@@ -955,8 +932,8 @@ bool encode_rows(void *encode, CUtensorMap *map, const int8_t *base, int64_t k, 
 }
 
 // Row tile, and blocks that share a tile: what takes the fewest cycles by a rough count.  A block of k costs 2.1 cycles for each
-// operand row; an epilogue 25 cycles a row and 50 more for every sixteen ranks (both measured at tiles of 256 rows), under the
-// next tile's products where there is one; starting, and joining the blocks that share a tile, a few thousand.
+// operand row; an epilogue 25 cycles a row and 25 more for every sixteen ranks (50 where the tile is split), under the next tile's
+// products where there is one; starting, and joining the blocks that share a tile, a few thousand.
 void plan(LinearParams &p, int n_sms)
 {
     p.tiles_m = (p.n + kTileM - 1) / kTileM;
@@ -1070,7 +1047,7 @@ extern "C" int isc_quant_linear(const int8_t *x, int64_t ldx, const float *x_sca
     p.rows = (int)rows; p.n = (int)n; p.k_blocks = (int)((k + kBlockK - 1) / kBlockK);
     p.vec_y = aligned(y, 16) && ldy * type_bytes(y_type) % 16 == 0;
     const cudaStream_t st = (cudaStream_t)cuda_stream;
-    const bool few = rows <= kFewRows, half = ad && ad->type == ISC_F16;
+    const bool half = ad && ad->type == ISC_F16;
     if (ad) {
         InnerParams q = {};
         q.x = x; q.a = ad->a; q.scale = ad->scale; q.ids = ad->ids;
@@ -1083,11 +1060,9 @@ extern "C" int isc_quant_linear(const int8_t *x, int64_t ldx, const float *x_sca
         p.b = ad->b; p.ids = ad->ids; p.inner = q.inner;
         p.rank = ad->rank; p.n_adapters = ad->n_adapters; p.adapter_type = ad->type;
     }
-    if (few) {
-        const FewParams f = {x, w, x_scale, w_scale, bias, p.inner, p.b, p.ids, y, ldx, ldw, ldy, p.rows, p.n, (int)k, p.rank, p.ranks, p.n_adapters, y_type};
-        void (*const kernel)(FewParams) = half ? k_quant_linear_few<1, 1, true> : k_quant_linear_few<1, 1, false>;
-        const int per_block = kFewThreads / 32;
-        e = launch(kernel, f, dim3((unsigned)((n + per_block - 1) / per_block)), kFewThreads, 0, 1, ad != nullptr, st);
+    if (rows == 1) {
+        const OneParams one = {x, w, x_scale, w_scale, bias, p.inner, p.b, p.ids, y, ldw, p.n, (int)k, p.rank, p.n_adapters, y_type};
+        e = launch(half ? k_quant_linear_one<true> : k_quant_linear_one<false>, one, dim3((unsigned)((n + kOneThreads / 32 - 1) / (kOneThreads / 32))), kOneThreads, 0, 1, ad != nullptr, st);
         return status_of(e, "quant_linear");
     }
     plan(p, dev.n_sms);
