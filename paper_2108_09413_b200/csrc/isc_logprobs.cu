@@ -224,7 +224,14 @@ template <typename T> __device__ __forceinline__ float largest(const Chunk<T> &e
 struct Own {
     float m = -INFINITY, seen = -INFINITY;      // seen: m, or NaN if there is one
     Pair s = 0, u = 0;
-    int best = 0;                       // the first chunk with the largest logit of its chunks
+    float top = -INFINITY;              // of the present subset of its chunks: the largest logit,
+    int best = 0;                       // the first chunk that has it
+    __device__ __forceinline__ Key subset()
+    {
+        const Key k = top > -INFINITY ? make_key(top, (uint32_t)best) : 0;
+        top = -INFINITY;
+        return k;
+    }
     __device__ __forceinline__ Sums sums() const
     {
         float a, b, x, y;
@@ -277,11 +284,12 @@ struct Own {
             all = sizeof(T) == 1 ? fmaxf(all, most[i]) : max_nan(all, most[i]);
         }
         if (sizeof(T) != 1) seen = max_nan(seen, all);
-        if (all > m) {
-            rise(all, c);
+        if (all > top) {
+            top = all;
 #pragma unroll
             for (int i = kN - 1; i >= 0; --i)
                 if (most[i] == all) best = first + i * stride;
+            if (all > m) rise(all, c);
         }
         if (m > (sizeof(T) == 2 ? Finite<T>::kMasked : -limit) && fabsf(m) < limit) {
             const Pair minus_m = make_pair(-m, -m), c2 = make_pair(c, c);
@@ -302,11 +310,11 @@ struct Own {
     }
 };
 
-template <int kWarps> struct Shared {
+template <int kWarps, int kSubsets = 1> struct Shared {
     Sums warp[kWarps];
     Sums block;                         // read by the cluster's other blocks
     int bad[kWarps], block_bad, n_candidates, n_chosen;
-    int chosen[32 * kWarps];            // first chunks of the subsets that hold the alternatives
+    int chosen[32 * kWarps * kSubsets]; // first chunks of the subsets that hold the alternatives
     Key group[32], found[kWarps];
     Key top[kMostTop];                  // read by the cluster's first block
     alignas(16) Key candidate[kCandidates];
@@ -342,7 +350,7 @@ __device__ __forceinline__ uint32_t read_remote(uint32_t addr)
 }
 
 // Every thread gets its team's sums.  `edge`: this thread's logit outside the chunks (minus infinity: none).
-template <int kWarps> __device__ __forceinline__ Sums join_all(Shared<kWarps> &sh, const Team &team, const Own &own, float edge, float c, bool &bad)
+template <int kWarps, int kSubsets> __device__ __forceinline__ Sums join_all(Shared<kWarps, kSubsets> &sh, const Team &team, const Own &own, float edge, float c, bool &bad)
 {
     Sums all = own.sums();
     if (edge > -INFINITY) all = join(all, Sums{edge, 1.0f, 0.0f}, c);
@@ -378,7 +386,7 @@ __device__ __forceinline__ void place_key(const Key (*sorted)[32], int lists, in
 }
 
 // Places of the `n` keys in `list` by counting the larger ones; the first `k` go to `top` (zero: none).
-template <int kWarps> __device__ void rank_candidates(Shared<kWarps> &sh, const Team &team, int n, int k)
+template <int kWarps, int kSubsets> __device__ void rank_candidates(Shared<kWarps, kSubsets> &sh, const Team &team, int n, int k)
 {
     if (team.t < kMostTop) sh.top[team.t] = 0;
     team.sync();
@@ -392,16 +400,19 @@ template <int kWarps> __device__ void rank_candidates(Shared<kWarps> &sh, const 
     team.sync();
 }
 
-// The k largest logits of this team's chunks and edges into sh.top; after join_all.  A thread's chunks are first, first + stride, ...
-template <typename T, int kWarps> __device__ void team_top(Shared<kWarps> &sh, const Team &team, const Row<T> &row, const Own &own, float edge, int edge_index, int first, int stride, int k)
+// The k largest logits of this team's chunks and edges into sh.top; after join_all.  A thread's chunks are first, first + stride, ...; its
+// subsets, `each` of them one after the other, have the keys `key`.
+template <typename T, int kWarps, int kSubsets>
+__device__ void team_top(Shared<kWarps, kSubsets> &sh, const Team &team, const Row<T> &row, const Key (&key)[kSubsets], float edge, int edge_index, int first, int stride, int each, int k)
 {
     const int t = team.t, lane = t & 31, warp = t >> 5, warps = team.threads >> 5;
     constexpr int kSize = Chunk<T>::kSize;
-    const Key key = own.m > -INFINITY ? make_key(own.m, (uint32_t)own.best) : 0;
     // The k-th largest of 32 groups' largest keys: k subsets at least reach it, and seldom many more (all of a warp's lanes
     // are a group each, k exactly).  A full order of the subsets' maxima took 1.5 us here.
     const int group = team.threads >> 5;
-    Key most = key;
+    Key most = 0;
+#pragma unroll
+    for (int s = 0; s < kSubsets; ++s) most = max(most, key[s]);
     for (int d = 1; d < group; d <<= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, d));
     if ((t & (group - 1)) == 0) sh.group[t / group] = most;
     if (t == 0) sh.n_chosen = 0;
@@ -412,14 +423,16 @@ template <typename T, int kWarps> __device__ void team_top(Shared<kWarps> &sh, c
     for (int j = 0; j < 32; ++j) larger += sh.group[j] > most;
     const uint32_t kth = __ballot_sync(0xffffffffu, most && larger == k - 1);
     const Key least = kth ? __shfl_sync(0xffffffffu, most, __ffs((int)kth) - 1) : 1;
-    if (key >= least) sh.chosen[atomicAdd(&sh.n_chosen, 1)] = first;
+#pragma unroll
+    for (int s = 0; s < kSubsets; ++s)
+        if (key[s] >= least) sh.chosen[atomicAdd(&sh.n_chosen, 1)] = first + s * each * stride;
     if (edge > -INFINITY) {
         const int at = atomicAdd(&sh.n_candidates, 1);
         sh.candidate[at] = make_key(edge, (uint32_t)edge_index);     // (the first few: there is room)
     }
     team.sync();
     // the chosen subsets' chunks, dealt out over all threads, four loads of a thread under way at once
-    const int each = (row.chunks + stride - 1) / stride, items = sh.n_chosen * each;
+    const int items = sh.n_chosen * each;
     for (int i0 = t; i0 < items; i0 += 4 * team.threads) {
         Chunk<T> e[4];
         int chunk[4];
@@ -478,7 +491,7 @@ template <typename T, int kWarps> __device__ void team_top(Shared<kWarps> &sh, c
 }
 
 // by one thread for each alternative at least
-template <int kWarps> __device__ __forceinline__ void write_results(const LogProbParams &p, const Shared<kWarps> &sh, const Given &given, int64_t row_index, Sums all, bool bad, int t)
+template <int kWarps, int kSubsets> __device__ __forceinline__ void write_results(const LogProbParams &p, const Shared<kWarps, kSubsets> &sh, const Given &given, int64_t row_index, Sums all, bool bad, int t)
 {
     const RowResult r = row_result(all, bad);
     if (t == 0) write_row(p, r, given, row_index);
@@ -512,7 +525,8 @@ template <typename T> __global__ void __launch_bounds__(kThreads) k_log_probs(co
     bool bad;
     Sums all = join_all(sh, team, own, edge, c, bad);
     const int k = max(p.top, p.votes ? 1 : 0);
-    if (k) team_top<T>(sh, team, row, own, edge, edge_index, first, stride, k);
+    const Key key[1] = {own.subset()};
+    if (k) team_top<T>(sh, team, row, key, edge, edge_index, first, stride, (row.chunks + stride - 1) / stride, k);
     if (p.cluster > 1) {
         if (t == 0) { sh.block = all; sh.block_bad = bad; }
         cluster_sync();
@@ -570,16 +584,18 @@ template <typename T> __global__ void __launch_bounds__(32 * kRowWarps) k_log_pr
     }
     bool bad;
     const Sums all = join_all(sh, team, own, edge, c, bad);
-    if (k) team_top<T>(sh, team, row, own, edge, edge_index, t, 32, k);
+    const Key key[1] = {own.subset()};
+    if (k) team_top<T>(sh, team, row, key, edge, edge_index, t, 32, (row.chunks + 31) / 32, k);
     write_results(p, sh, given, r, all, bad, t);
 }
 
 // many rows: eight warps that work and one that copies
-constexpr int kStreamThreads = 256, kPieces = 4, kPieceBytes = 16384, kStreamBlocks = 3;
+static_assert(kCandidates >= 512, "two keys for each thread");
+constexpr int kStreamThreads = 256, kPieces = 4, kPieceBytes = 16384, kStreamBlocks = 3, kStreamSubsets = 2;
 template <typename T> __global__ void __launch_bounds__(kStreamThreads + 32, kStreamBlocks) k_log_probs_stream(const __grid_constant__ LogProbParams p)
 {
     extern __shared__ __align__(128) uint8_t pieces[];
-    __shared__ Shared<kStreamThreads / 32> sh;
+    __shared__ Shared<kStreamThreads / 32, kStreamSubsets> sh;
     __shared__ __align__(8) uint64_t full[kPieces], empty[kPieces];
     __shared__ int failed;
     if (threadIdx.x == 0) {
@@ -623,28 +639,40 @@ template <typename T> __global__ void __launch_bounds__(kStreamThreads + 32, kSt
         const float edge = edge_index >= 0 ? to_float(row.at[edge_index]) : -INFINITY;
         const Given given = given_of(p, row.at, r, t == 0);
         Own own;
+        // two subsets a thread: what is read again for the alternatives is half.  Their keys wait where the candidates will be: there
+        // are no registers for them
+        const int n_pieces = (row.chunks + kPieceChunks - 1) / kPieceChunks, per_subset = (n_pieces + kStreamSubsets - 1) / kStreamSubsets, each = per_subset * (kPieceChunks / kStreamThreads);
+        int left_in_subset = per_subset, at_subset = t;
+        sh.candidate[t + kStreamThreads] = 0;
         for (int from = 0; from < row.chunks; from += kPieceChunks) {
             if (!wait_limited(tc::smem_u32(&full[slot]), (uint32_t)use & 1u, &failed)) { timeout_word = 1; own.seen = NAN; }
             const int left = row.chunks - from - t;
-            constexpr int kN = kPieceChunks / kStreamThreads;
-            Chunk<T> e[kN];
-#pragma unroll
-            for (int i = 0; i < kN; ++i) e[i] = *reinterpret_cast<const Chunk<T> *>(pieces + slot * kPieceBytes + 16 * (i * kStreamThreads + t));
-            if (left > (kN - 1) * kStreamThreads && sizeof(T) > 1) own.add(e, kN, from + t, kStreamThreads, c, p.limit);
-            else if (sizeof(T) == 1) {
+            // (int8: one chunk has 16 logits, and there are no registers for more)
+            constexpr int kN = kPieceChunks / kStreamThreads, kTogether = sizeof(T) == 1 ? 1 : kN;
 #pragma unroll 1
-                for (int i = 0; i < kN && left > i * kStreamThreads; ++i) {
-                    const Chunk<T> one[1] = {*reinterpret_cast<const Chunk<T> *>(pieces + slot * kPieceBytes + 16 * (i * kStreamThreads + t))};
-                    own.add(one, 1, from + i * kStreamThreads + t, kStreamThreads, c, p.limit);
-                }
-            } else if (left > 0) own.add(e, (left + kStreamThreads - 1) / kStreamThreads, from + t, kStreamThreads, c, p.limit);
+            for (int i0 = 0; i0 < kN; i0 += kTogether) {
+                Chunk<T> e[kTogether];
+#pragma unroll
+                for (int i = 0; i < kTogether; ++i) e[i] = *reinterpret_cast<const Chunk<T> *>(pieces + slot * kPieceBytes + 16 * ((i0 + i) * kStreamThreads + t));
+                const int here = left - i0 * kStreamThreads;
+                if (here > (kTogether - 1) * kStreamThreads) own.add(e, kTogether, from + i0 * kStreamThreads + t, kStreamThreads, c, p.limit);
+                else if (here > 0) own.add(e, (here + kStreamThreads - 1) / kStreamThreads, from + i0 * kStreamThreads + t, kStreamThreads, c, p.limit);
+            }
             __syncwarp();
             if ((t & 31) == 0) tc::mbar_arrive(tc::smem_u32(&empty[slot]));
             if (++slot == kPieces) { slot = 0; ++use; }
+            if (--left_in_subset == 0 || from + kPieceChunks >= row.chunks) {
+                sh.candidate[at_subset] = own.subset();
+                at_subset += kStreamThreads;
+                left_in_subset = per_subset;
+            }
         }
         bool bad;
         const Sums all = join_all(sh, team, own, edge, c, bad);
-        if (k) team_top<T>(sh, team, row, own, edge, edge_index, t, kStreamThreads, k);
+        if (k) {
+            const Key key[kStreamSubsets] = {sh.candidate[t], sh.candidate[t + kStreamThreads]};
+            team_top<T>(sh, team, row, key, edge, edge_index, t, kStreamThreads, each, k);
+        }
         write_results(p, sh, given, r, all, bad, t);
         team.sync();
     }
@@ -749,7 +777,8 @@ template <typename T> cudaError_t launch_log_probs(const Device &dev, LogProbPar
         return cudaGetLastError();
     }
     const int chunks = (int)(p.vocab * (int64_t)sizeof(T) / 16);
-    const int threads = chunks >= 4 * kThreads ? kThreads : chunks >= 2 * kThreads ? kThreads / 2 : kThreads / 4;
+    // (more rows than SMs: smaller blocks, so that all are at work at once)
+    const int threads = chunks >= 4 * kThreads && p.rows <= dev.n_sms ? kThreads : chunks >= 2 * kThreads ? kThreads / 2 : kThreads / 4;
     p.cluster = 1;
     while (p.cluster < kMostCluster && p.rows * p.cluster * 2 <= 4 * dev.n_sms && chunks >= 4 * threads * p.cluster) p.cluster *= 2;
     cudaLaunchAttribute attr;
