@@ -399,7 +399,7 @@ typedef enum { ISC_BF16 = 0, ISC_F16 = 1, ISC_F32 = 2, ISC_I8 = 3 } isc_type;
  *   q           : [rows][width] int8, pitch ldq (a multiple of 16 for isc_quant_linear; bytes behind the row's end are
  *                 left as they are).      scale : [rows].
  * A row of zeros has scale 0 and codes 0; a row with an infinity or NaN in h or p has scale NaN and codes 0.
- * Errors: ISC_ERR_ARG, ISC_ERR_UNSUPPORTED (2^31 rows or elements of a row and more), ISC_ERR_CUDA.
+ * Errors: ISC_ERR_ARG, ISC_ERR_UNSUPPORTED (2^31 rows, 2^31 - 8,192 elements of a row and more), ISC_ERR_CUDA.
  */
 int isc_rms_norm_quant(const void *x, int64_t ldx, const void *residual, int64_t ldr, const void *weight, int weight_type,
                        int type, int64_t rows, int64_t width, float eps, void *sum, int64_t lds, int8_t *q, int64_t ldq,
@@ -445,7 +445,8 @@ int isc_quant_linear_work_space(int64_t rows, int rank, int64_t *out_bytes);
  * A logit of minus infinity is masked: probability 0, never an alternative.  Where a row has fewer than `top` others, the
  * rest of its alternatives has id -1 and log probability -inf.  A row with nothing but masks has log probability -inf,
  * entropy 0 and no vote.  A row with a NaN or plus infinity has NaN results, ids -1 and no vote.
- * Sums are held in single precision.  Errors: ISC_ERR_ARG, ISC_ERR_UNSUPPORTED (2^31 rows or columns), ISC_ERR_CUDA.
+ * Sums are held in single precision; a log probability below its range is minus infinity.
+ * Errors: ISC_ERR_ARG, ISC_ERR_UNSUPPORTED (2^28 rows, 2^30 columns and more), ISC_ERR_CUDA.
  */
 int isc_log_probs(const void *logits, int64_t ld, int type, int64_t rows, int64_t vocab, float scale,
                   const int64_t *targets, int top, float *out_log_probs, float *out_entropy, int32_t *out_top_ids,

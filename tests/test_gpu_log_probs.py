@@ -43,7 +43,8 @@ def definition(logits, targets, top, scale):
 
 
 def close(got, exact, tolerance):
-    got, exact = got.double().cpu(), exact
+    # (1.3 times the lowest bfloat16 is -4.4e38: no single-precision number but minus infinity is near it)
+    got, exact = got.double().cpu(), torch.where(exact < -3.4028235677973366e38, -math.inf, exact)
     fine = torch.isfinite(exact)
     assert torch.equal(torch.isnan(got), torch.isnan(exact))
     assert torch.equal(got[~fine & ~torch.isnan(exact)], exact[~fine & ~torch.isnan(exact)])
@@ -138,6 +139,28 @@ def test_large_logits_in_one_thread_s_share(vocab):
     x = torch.stack(rows)
     for r in (x, x[2:3], x.expand(9, vocab).repeat(40, 1)):
         check(r, None, 32)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp16", "fp32", "int8"])
+@pytest.mark.parametrize("vocab,pad", [(17001, 0), (20480, 16), (70003, 5)])
+def test_many_long_rows(kind, vocab, pad):
+    """More rows than blocks: each block's copies run on from row to row, over rows of every sort."""
+    g = torch.Generator(device="cuda").manual_seed(vocab)
+    rows = 900
+    x = torch.randn(rows, vocab + pad, device="cuda", generator=g) * (30.0 if kind == "int8" else 3.0)
+    x[::7] = x[::7].round()                                    # many ties
+    x[3::50] = 1.0                                             # nothing but ties: more candidates than there is room for
+    x[4::50] = torch.where(torch.arange(vocab + pad, device="cuda") // (16 if kind == "int8" else 8) % 512 < 1, 20.0, 0.0)
+    if kind != "int8":
+        x[5::50] = -math.inf
+        x[6::50, vocab // 2:] = -math.inf
+        x[8::50, vocab - 1] = math.nan
+        x[9::50, 0] = math.inf
+        x[10::50] = torch.finfo(TYPES[kind]).min
+        x[11::50, torch.rand(vocab + pad, device="cuda", generator=g) < 0.999] = torch.finfo(TYPES[kind]).min
+    x = (x.round().clamp(-128, 127) if kind == "int8" else x).to(TYPES[kind])[:, :vocab]
+    for top in (0, 3, 32):
+        check(x, some_targets(rows, vocab, g), top, 0.1 if kind == "int8" else 1.3)
 
 
 def test_zero_rows_and_parts_not_asked_for():

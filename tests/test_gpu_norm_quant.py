@@ -109,6 +109,36 @@ def test_rows_at_the_ends_of_the_range(kind, width, eps):
     assert torch.isnan(scale).all() and not q.any()
 
 
+@pytest.mark.parametrize("kind", ["bf16", "fp16", "fp32"])
+@pytest.mark.parametrize("rows,width", [(5000, 1032), (2600, 2048), (1301, 4096), (700, 8192), (400, 16384)])
+@pytest.mark.parametrize("pad", [0, 8])
+def test_many_rows(kind, rows, width, pad):
+    """More rows than teams: rows are brought ahead, among them rows of every sort, with the sum in place and without a residual."""
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    dtype = TYPES[kind]
+    top = torch.finfo(dtype).max
+    x, r = (3 * torch.randn(rows, width, device="cuda", generator=g) for _ in range(2))
+    for t in (x, r):
+        t[1::40] = 0.0
+        t[3::40, 7] = float("inf")
+        t[4::40, width - 1] = float("nan")
+        t[6::40] *= torch.finfo(dtype).smallest_normal * 4
+    x[5::40] = -top / 2
+    x[8::40] = (torch.randint(-127, 127, (width,), device="cuda", generator=g) + 0.5) * 0.25     # quotients between two codes
+    x[8::40, width // 2] = 31.75
+    r[8::40] = 0.0
+    x, r = rows_of(x.to(dtype), pad), rows_of(r.to(dtype), pad)
+    w = (1 + 0.2 * torch.randn(width, device="cuda", generator=g))
+    check(isc.rms_norm_quant(x, w.to(dtype), EPS), x, None, w.to(dtype))
+    check(isc.rms_norm_quant(x, torch.ones_like(w), EPS, residual=r), x, r, torch.ones_like(w))
+    kept = r.clone()
+    got = isc.rms_norm_quant(x, w, EPS, residual=r, sum_out=r)
+    check(got, x, kept, w)
+    again = isc.rms_norm_quant(x, w, EPS, residual=kept)
+    for a, b in zip(got, again):
+        assert torch.equal(a.nan_to_num(1.0), b.nan_to_num(1.0))
+
+
 def test_sum_that_leaves_its_type():
     x = torch.full((2, 40), 60000.0, device="cuda", dtype=torch.float16)
     w = torch.ones(40, device="cuda", dtype=torch.float16)
