@@ -74,6 +74,8 @@ def _enqueue(what, device, stream, call):
     """`call(raw stream)`, a status, with the tensors' device and `stream` current."""
     torch = _torch
     index = device.index
+    if stream is not None and stream.device_index != index:
+        _refuse(what, "the stream belongs to another device than the tensors")
     if stream is None and index == torch.cuda.current_device():
         rc = call(torch._C._cuda_getCurrentRawStream(index))
     else:

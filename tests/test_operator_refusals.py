@@ -100,3 +100,12 @@ def test_tensors_of_the_host_are_refused():
         with pytest.raises(isc.IscError) as e:
             call()
         assert e.value.code == ARG
+
+
+def test_a_stream_of_another_device_is_refused():
+    from types import SimpleNamespace
+    from paper_2108_09413_b200 import operators
+    operators._start()
+    with pytest.raises(isc.IscError) as e:
+        operators._enqueue("isc_log_probs", torch.device("cuda", 0), SimpleNamespace(device_index=1), lambda raw: pytest.fail("went through"))
+    assert e.value.code == ARG
