@@ -177,7 +177,10 @@ def quant_linear(x, x_scale, w, w_scale, bias=None, adapters=None, adapter_ids=N
         if y is None:
             y = _empty((rows, n), dtype, device)
         work = _empty((space,), torch.uint8, device) if space else None
-        return lib().isc_quant_linear(x.data_ptr(), ldx, x_scale.data_ptr(), rows, w.data_ptr(), ldw, w_scale.data_ptr(), k, n, _ptr(bias),
+        factors = x_scale
+        if adapters is not None and parts is None:      # no adapter at all: every id that is not negative is too large
+            factors = torch.where(adapter_ids < 0, x_scale, float("nan"))
+        return lib().isc_quant_linear(x.data_ptr(), ldx, factors.data_ptr(), rows, w.data_ptr(), ldw, w_scale.data_ptr(), k, n, _ptr(bias),
                                       C.addressof(parts) if parts is not None else None, y.data_ptr(), y.stride(0) if rows > 1 else n, code,
                                       _ptr(work), space, raw)
     _enqueue("isc_quant_linear", device, stream, call)

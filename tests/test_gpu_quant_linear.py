@@ -182,3 +182,13 @@ def test_zero_rows_and_no_adapters_at_all():
     none = (torch.zeros(0, 8, 64, device="cuda").half(), torch.zeros(0, 50, 8, device="cuda").half(), torch.zeros(0, device="cuda"))
     ids = torch.full((4,), -1, dtype=torch.int32, device="cuda")
     assert torch.equal(call(s), isc.quant_linear(s["x"], s["x_scale"], s["w"], s["w_scale"], adapters=none, adapter_ids=ids))
+
+
+def test_ids_without_adapters_are_too_large():
+    """A row whose id is the number of adapters or more is NaN, with no adapters too."""
+    for rows in (1, 4, 300):
+        s = problem(rows, 64, 50)
+        none = (torch.zeros(0, 8, 64, device="cuda").half(), torch.zeros(0, 50, 8, device="cuda").half(), torch.zeros(0, device="cuda"))
+        ids = torch.arange(rows, dtype=torch.int32, device="cuda") % 2 - 1
+        y, plain = isc.quant_linear(s["x"], s["x_scale"], s["w"], s["w_scale"], adapters=none, adapter_ids=ids), call(s)
+        assert torch.equal(y[ids < 0], plain[ids < 0]) and torch.isnan(y[ids >= 0]).all()
