@@ -1,8 +1,9 @@
 """The library's operators on device tensors (the last part of include/isc.h) for torch tensors.
 
 Every call checks its arguments, allocates its outputs and enqueues one of the library's operators on `stream` (a torch
-stream; the current one of the tensors' device by default).  Outputs belong to that stream.  The operators compute no
-gradients: inputs that require one are refused while gradients are enabled.
+stream; the current one of the tensors' device by default).  Outputs belong to that stream; inputs may be dropped after the
+call, whichever stream they belong to.  The operators compute no gradients: inputs that require one are refused while
+gradients are enabled.
 """
 from __future__ import annotations
 
@@ -70,8 +71,9 @@ def _empty(shape, dtype, device):
     return _torch.empty_strided(shape, (shape[1], 1) if len(shape) == 2 else (1,), dtype=dtype, device=device)
 
 
-def _enqueue(what, device, stream, call):
-    """`call(raw stream)`, a status, with the tensors' device and `stream` current."""
+def _enqueue(what, device, stream, call, tensors=()):
+    """`call(raw stream)`, a status, with the tensors' device and `stream` current.  The memory of `tensors` (or None), which may be
+    another stream's, is not given to others before `stream` has used it."""
     torch = _torch
     index = device.index
     if stream is not None and stream.device_index != index:
@@ -81,6 +83,10 @@ def _enqueue(what, device, stream, call):
     else:
         with torch.cuda.device(index), torch.cuda.stream(stream if stream is not None else torch.cuda.current_stream(index)):
             rc = call(torch._C._cuda_getCurrentRawStream(index))
+        if stream is not None:
+            for t in tensors:
+                if t is not None and t.numel():
+                    t.record_stream(stream)
     if rc != 0:
         raise IscError(rc, what)
 
@@ -95,7 +101,8 @@ def rms_norm_quant(x, weight, eps=1e-6, residual=None, sum_out=None, stream=None
     """
     torch = _torch or _start()
     what = "rms_norm_quant"
-    device = _same_device(what, (x, weight, residual, sum_out))
+    given = (x, weight, residual, sum_out)
+    device = _same_device(what, given)
     dtype, shape = x.dtype, x.shape
     code = _types.get(dtype, 3)
     if code == 3:
@@ -117,7 +124,7 @@ def rms_norm_quant(x, weight, eps=1e-6, residual=None, sum_out=None, stream=None
         scale = _empty((rows,), torch.float32, device)
         return lib().isc_rms_norm_quant(x.data_ptr(), ldx, _ptr(residual), ldr, weight.data_ptr(), 2 if wide else code, code, rows, width, eps,
                                         _ptr(total), total.stride(0) if total is not None and rows > 1 else width, q.data_ptr(), pitch, scale.data_ptr(), raw)
-    _enqueue("isc_rms_norm_quant", device, stream, call)
+    _enqueue("isc_rms_norm_quant", device, stream, call, given)
     return (q if pitch == width else q[:, :width]), scale, total
 
 
@@ -138,7 +145,8 @@ def quant_linear(x, x_scale, w, w_scale, bias=None, adapters=None, adapter_ids=N
     torch = _torch or _start()
     what = "quant_linear"
     a, b, factor = adapters if adapters is not None else (None, None, None)
-    device = _same_device(what, (x, x_scale, w, w_scale, bias, a, b, factor, adapter_ids, out))
+    given = (x, x_scale, w, w_scale, bias, a, b, factor, adapter_ids, out)
+    device = _same_device(what, given)
     ldx, ldw = _pitch(what, "x", x, torch.int8), _pitch(what, "w", w, torch.int8)
     rows, k = x.shape
     n = w.shape[0]
@@ -183,7 +191,7 @@ def quant_linear(x, x_scale, w, w_scale, bias=None, adapters=None, adapter_ids=N
         return lib().isc_quant_linear(x.data_ptr(), ldx, factors.data_ptr(), rows, w.data_ptr(), ldw, w_scale.data_ptr(), k, n, _ptr(bias),
                                       C.addressof(parts) if parts is not None else None, y.data_ptr(), y.stride(0) if rows > 1 else n, code,
                                       _ptr(work), space, raw)
-    _enqueue("isc_quant_linear", device, stream, call)
+    _enqueue("isc_quant_linear", device, stream, call, given)
     return y
 
 
@@ -219,5 +227,5 @@ def log_probs(logits, targets=None, top=0, scale=1.0, votes=None, entropy=True, 
             alternatives = _empty((rows, top), numbers, device)
         return lib().isc_log_probs(logits.data_ptr(), ld, code, rows, vocab, scale, _ptr(targets), top, _ptr(given), _ptr(h), _ptr(ids),
                                    _ptr(alternatives), _ptr(votes), raw)
-    _enqueue("isc_log_probs", device, stream, call)
+    _enqueue("isc_log_probs", device, stream, call, (logits, targets, votes))
     return given, h, ids, alternatives
