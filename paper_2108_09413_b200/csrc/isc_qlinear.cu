@@ -1013,6 +1013,7 @@ cudaError_t linear_take_timeout(cudaStream_t st, bool *expired) { return take_ti
 extern "C" int isc_quant_linear_work_space(int64_t rows, int rank, int64_t *out_bytes)
 {
     if (rows < 0 || rank < 0 || rank > 128 || !out_bytes) return ISC_ERR_ARG;
+    if (rows >= INT32_MAX / 2) return ISC_ERR_UNSUPPORTED;
     *out_bytes = isc::work_bytes_of(rows, rank);
     return ISC_OK;
 }
@@ -1031,7 +1032,7 @@ extern "C" int isc_quant_linear(const int8_t *x, int64_t ldx, const float *x_sca
         if (!ad->a || !ad->b || !ad->scale || !ad->ids || ad->n_adapters < 1 || ad->rank < 1 || (ad->type != ISC_BF16 && ad->type != ISC_F16)) return ISC_ERR_ARG;
         if (!aligned(ad->scale, 4) || !aligned(ad->ids, 4) || !work || !aligned(work, 16)) return ISC_ERR_ARG;
         if (ad->rank % 4 || ad->rank > 128 || !aligned(ad->a, 16) || !aligned(ad->b, 16)) return ISC_ERR_UNSUPPORTED;
-        if (work_bytes < isc::work_bytes_of(rows, ad->rank)) return ISC_ERR_ARG;
+        if (rows < INT32_MAX / 2 && work_bytes < isc::work_bytes_of(rows, ad->rank)) return ISC_ERR_ARG;
     }
     // a single row has no pitch
     if (rows == 1) ldx = (k + 15) & ~(int64_t)15;

@@ -109,3 +109,14 @@ def test_a_stream_of_another_device_is_refused():
     with pytest.raises(isc.IscError) as e:
         operators._enqueue("isc_log_probs", torch.device("cuda", 0), SimpleNamespace(device_index=1), lambda raw: pytest.fail("went through"))
     assert e.value.code == ARG
+
+
+def test_more_rows_than_the_work_space_s_size_can_tell():
+    from paper_2108_09413_b200.operators import _Adapters
+    size = C.c_int64(7)
+    for rows in (2**30, 2**56, 2**62):
+        assert isc.lib().isc_quant_linear_work_space(rows, 128, C.byref(size)) == UNSUPPORTED and size.value == 7
+        parts = _Adapters(AT, AT, AT, AT, 0, 4, 128)
+        good = list(LINEAR_GOOD)
+        good[LINEAR["adapters"]], good[LINEAR["rows"]] = C.addressof(parts), rows
+        assert isc.lib().isc_quant_linear(*good) == UNSUPPORTED
