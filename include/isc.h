@@ -420,7 +420,7 @@ int isc_rms_norm_quant(const void *x, int64_t ldx, const void *residual, int64_t
  *              time (or two graphs that hold one and run at once) need two.
  * The int8 products are summed exactly; the adapters' sums are held in single precision.
  * Requirements, else ISC_ERR_UNSUPPORTED: x, w, a, b 16 bytes aligned, ldx and ldw multiples of 16; k <= 65,536; rank a
- * multiple of 4 up to 128; rows and n below 2^31 / 2.  Other errors: ISC_ERR_ARG, ISC_ERR_CUDA.
+ * multiple of 4 up to 128; rows and n below 2^30 - 1.  Other errors: ISC_ERR_ARG, ISC_ERR_CUDA.
  */
 typedef struct {
     const void *a, *b;

@@ -55,8 +55,6 @@ struct NormParams {
 
 struct Sums { float ss, most; };
 
-__device__ __forceinline__ Sums combine(Sums a, Sums b) { return Sums{a.ss + b.ss, max_nan(a.most, b.most)}; }
-
 template <typename T> __device__ __forceinline__ float weight_at(const NormParams &p, int i)
 {
     return p.wide_w ? __ldg(static_cast<const float *>(p.w) + i) : to_float(static_cast<const T *>(p.w)[i]);
@@ -99,7 +97,7 @@ template <typename T> __device__ __forceinline__ void fetch_weights(const NormPa
     }
 }
 
-// the exact product, or its nearest double-precision number
+// x + r in double precision: exact unless their exponents lie far apart
 template <typename T> __device__ __forceinline__ double exact_sum(T x, T r, bool has_r) { return has_r ? (double)to_float(x) + (double)to_float(r) : (double)to_float(x); }
 
 // Where single precision leaves no doubt about anything but codes next to the middle between two: the range in which the sums

@@ -50,7 +50,7 @@ template <typename Word> cudaError_t take_timeout(const Word &device_word, cudaS
 }
 
 // Eight elements as they lie in memory.
-template <typename T> struct alignas(sizeof(T) == 1 ? 8 : 16) Eight { T v[8]; };
+template <typename T> struct alignas(16) Eight { T v[8]; };
 
 // once-read data: past the first-level cache
 template <typename T> __device__ __forceinline__ Eight<T> load_eight(const T *p)
@@ -107,7 +107,6 @@ __device__ __forceinline__ Pair pair_of(const Eight<__nv_bfloat16> &e, int i)
     const uint32_t w = reinterpret_cast<const uint32_t *>(&e)[i];
     return make_pair(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u));
 }
-__device__ __forceinline__ Pair pair_of(const Eight<int8_t> &e, int i) { return make_pair((float)e.v[2 * i], (float)e.v[2 * i + 1]); }
 __device__ __forceinline__ void put_pair(Eight<float> &e, int i, Pair p) { split(p, e.v[2 * i], e.v[2 * i + 1]); }
 __device__ __forceinline__ void put_pair(Eight<__half> &e, int i, Pair p)
 {

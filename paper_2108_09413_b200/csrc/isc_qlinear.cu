@@ -37,8 +37,6 @@
 #include <stdint.h>
 
 #include <algorithm>
-#include <cstdio>
-#include <cstdlib>
 
 #include "isc_conv.cuh"
 #include "isc_ops.cuh"
@@ -85,7 +83,7 @@ struct LinearParams {
     const float *inner;                 // [row][ranks]: inner sums times the adapter's scale, zeros behind its rank
     void *y;
     int64_t ldy;
-    int rows, n, k_blocks, rank, ranks, n_adapters, adapter_type, y_type;    // ranks: rank in whole sixteens
+    int rows, n, k_blocks, rank, ranks, n_adapters, y_type;    // ranks: rank in whole sixteens
     int tile_n, tiles_m, tiles_n, split, stages;
     uint32_t ring_bytes, acc_stride;    // shared memory of the stages; tensor-memory columns of an accumulator
     bool vec_y;
@@ -167,14 +165,14 @@ struct Strip {
     }
 };
 
-// kE x 8 rows as a lane of an epilogue warp meets them: it has rows row0 + 8 e + 2 (lane mod 4) + j.
-template <int kE> struct Rows {
-    int id[kE][2];
-    float scale[kE][2];
+// 16 rows as a lane of an epilogue warp meets them: it has rows row0 + 8 e + 2 (lane mod 4) + j.
+struct Rows {
+    int id[2][2];
+    float scale[2][2];
     template <bool kAdapters> __device__ __forceinline__ void load(const LinearParams &p, int row0, int lane)
     {
 #pragma unroll
-        for (int e = 0; e < kE; ++e)
+        for (int e = 0; e < 2; ++e)
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
                 const int row = row0 + 8 * e + 2 * (lane & 3) + j;
@@ -215,14 +213,14 @@ template <bool kHalf> __device__ __forceinline__ Pair widen_pair(uint32_t w)
 }
 
 // Sums of products over ranks, even and odd ones apart.
-template <int kE> struct Outer {
-    Pair v[4][kE][2];
+struct Outer {
+    Pair v[4][2][2];
     __device__ __forceinline__ void clear()
     {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
-            for (int e = 0; e < kE; ++e) v[i][e][0] = v[i][e][1] = 0;
+            for (int e = 0; e < 2; ++e) v[i][e][0] = v[i][e][1] = 0;
     }
     // sixteen ranks of all rows (kOne < 0) or of row kOne alone; inner(e, j, q): four inner sums of a row
     template <bool kHalf, int kOne, typename Inner> __device__ __forceinline__ void add(const Left &left, Inner inner)
@@ -233,7 +231,7 @@ template <int kE> struct Outer {
 #pragma unroll
             for (int i = 0; i < 4; ++i) { b[i][0] = widen_pair<kHalf>(left.v[i][q].x); b[i][1] = widen_pair<kHalf>(left.v[i][q].y); }
 #pragma unroll
-            for (int e = 0; e < kE; ++e)
+            for (int e = 0; e < 2; ++e)
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
                     if (kOne >= 0 && kOne != 2 * e + j) continue;
@@ -253,7 +251,7 @@ template <int kE> struct Outer {
 };
 
 // one row of several in a strip: its own adapter's ranks
-template <bool kHalf, int kE, int kOne, typename Inner> __device__ __forceinline__ void add_own(const LinearParams &p, const Rows<kE> &rows, int n0, int block, int lane, Inner inner, Outer<kE> &outer)
+template <bool kHalf, int kOne, typename Inner> __device__ __forceinline__ void add_own(const LinearParams &p, const Rows &rows, int n0, int block, int lane, Inner inner, Outer &outer)
 {
     const int a = rows.id[kOne >> 1][kOne & 1];
     if ((unsigned)a >= (unsigned)p.n_adapters) return;
@@ -261,14 +259,12 @@ template <bool kHalf, int kE, int kOne, typename Inner> __device__ __forceinline
     left.load(p, a, n0, block, lane);
     outer.template add<kHalf, kOne>(left, inner);
 }
-template <bool kHalf, int kE, typename Inner> __device__ __forceinline__ void add_each(const LinearParams &p, const Rows<kE> &rows, int n0, int block, int lane, Inner inner, Outer<kE> &outer)
+template <bool kHalf, typename Inner> __device__ __forceinline__ void add_each(const LinearParams &p, const Rows &rows, int n0, int block, int lane, Inner inner, Outer &outer)
 {
-    add_own<kHalf, kE, 0>(p, rows, n0, block, lane, inner, outer);
-    add_own<kHalf, kE, 1>(p, rows, n0, block, lane, inner, outer);
-    if constexpr (kE > 1) {
-        add_own<kHalf, kE, 2>(p, rows, n0, block, lane, inner, outer);
-        add_own<kHalf, kE, 3>(p, rows, n0, block, lane, inner, outer);
-    }
+    add_own<kHalf, 0>(p, rows, n0, block, lane, inner, outer);
+    add_own<kHalf, 1>(p, rows, n0, block, lane, inner, outer);
+    add_own<kHalf, 2>(p, rows, n0, block, lane, inner, outer);
+    add_own<kHalf, 3>(p, rows, n0, block, lane, inner, outer);
 }
 
 // Results of 32 outputs x 8 rows (f: outputs lane / 4 + 8 i, rows row0 + 2 (lane mod 4) + j) to y.  `staging`: this warp's.
@@ -324,8 +320,8 @@ __device__ __forceinline__ void store_rows(const LinearParams &p, const Strip &s
 }
 
 // The sums' scales, the adapters' part and the offset.  acc: fragments of 16 outputs each, e: which eight rows.
-template <bool kAdapters, int kE> __device__ __forceinline__ void finish(const LinearParams &p, const Strip &s, const Rows<kE> &rows, const Outer<kE> &outer, int row0, int e, int lane,
-                                                                        const int (&acc)[2][4], uint32_t staging)
+template <bool kAdapters> __device__ __forceinline__ void finish(const LinearParams &p, const Strip &s, const Rows &rows, const Outer &outer, int row0, int e, int lane,
+                                                                const int (&acc)[2][4], uint32_t staging)
 {
     float f[4][2];
 #pragma unroll
@@ -575,7 +571,7 @@ template <Form kForm, bool kAdapters, bool kHalf> __global__ void __launch_bound
             for (int tile = first_tile; tile < tiles; tile += tile_step, ++j) {
                 const int buf = j & 1, m0 = tile % p.tiles_m * kTileM, n0 = tile / p.tiles_m * p.tile_n;
                 strip.load(p, m0 + 32 * quarter, lane);
-                Rows<2> rows;
+                Rows rows;
                 rows.load<kAdapters>(p, n0 + 16 * half, lane);
                 int kept = -1;
                 if (kAdapters) {
@@ -613,9 +609,9 @@ template <Form kForm, bool kAdapters, bool kHalf> __global__ void __launch_bound
                     int v[2][8];
                     tmem_ld_frag(acc + 16u * (uint32_t)q, v[0]);
                     tmem_ld_frag(acc + (16u << 16) + 16u * (uint32_t)q, v[1]);
-                    Rows<2> next;
+                    Rows next;
                     next.load<kAdapters>(p, row0 + 32, lane);
-                    Outer<2> outer;
+                    Outer outer;
                     if (kAdapters) {
                         outer.clear();
                         const int a = rows.id[0][0];
@@ -625,7 +621,7 @@ template <Form kForm, bool kAdapters, bool kHalf> __global__ void __launch_bound
 #pragma unroll 1
                         for (int r = 0; r < p.ranks >> 4; ++r, from += 64) {
                             const auto inner = [&](int e, int jj, int quad) { return *reinterpret_cast<const float4 *>(from + (uint32_t)(8 * e + jj) * in_pitch + 16u * (uint32_t)quad); };
-                            if (!same) add_each<kHalf, 2>(p, rows, strip.n0, r, lane, inner, outer);
+                            if (!same) add_each<kHalf>(p, rows, strip.n0, r, lane, inner, outer);
                             else if ((unsigned)a < (unsigned)p.n_adapters) {
                                 Left left;
                                 if (a == kept) load_kept(left, left_s + (uint32_t)(32 * quarter) * b_pitch, b_pitch, r, lane);
@@ -639,7 +635,7 @@ template <Form kForm, bool kAdapters, bool kHalf> __global__ void __launch_bound
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
                         const int part[2][4] = {{v[0][4 * e], v[0][4 * e + 1], v[0][4 * e + 2], v[0][4 * e + 3]}, {v[1][4 * e], v[1][4 * e + 1], v[1][4 * e + 2], v[1][4 * e + 3]}};
-                        if (row0 + 8 * e < p.rows) finish<kAdapters, 2>(p, strip, rows, outer, row0, e, lane, part, mine);
+                        if (row0 + 8 * e < p.rows) finish<kAdapters>(p, strip, rows, outer, row0, e, lane, part, mine);
                     }
                     rows = next;
                 }
@@ -846,7 +842,7 @@ template <bool kHalf, int kRowBlocks, int kRankBlocks> __global__ void __launch_
                     ar[r][h] = rank < p.rank ? static_cast<const uint16_t *>(p.a) + ((int64_t)a * p.rank + rank) * p.k : nullptr;
                 }
             const int lo = chunk0 + (int)((int64_t)(chunk1 - chunk0) * share / shares), hi = chunk0 + (int)((int64_t)(chunk1 - chunk0) * (share + 1) / shares);
-constexpr int kAhead = kRankBlocks * kRowBlocks == 1 ? 4 : 2;
+            constexpr int kAhead = kRankBlocks * kRowBlocks == 1 ? 4 : 2;
 #pragma unroll kAhead
             for (int ch = lo; ch < hi; ++ch) {
                 const int k0 = 64 * ch + 16 * c;
@@ -1059,7 +1055,7 @@ extern "C" int isc_quant_linear(const int8_t *x, int64_t ldx, const float *x_sca
         e = launch_inner(q, ad->type, dev.n_sms, st);
         if (e != cudaSuccess) return status_of(e, "quant_linear, inner sums");
         p.b = ad->b; p.ids = ad->ids; p.inner = q.inner;
-        p.rank = ad->rank; p.n_adapters = ad->n_adapters; p.adapter_type = ad->type;
+        p.rank = ad->rank; p.n_adapters = ad->n_adapters;
     }
     if (rows == 1) {
         const OneParams one = {x, w, x_scale, w_scale, bias, p.inner, p.b, p.ids, y, ldw, p.n, (int)k, p.rank, p.n_adapters, y_type};
