@@ -455,12 +455,14 @@ template <bool kAdapters> __device__ __forceinline__ void finish_part(const Line
 }
 
 // The adapters' operands of a block's first tile into the second-level cache: what a call of few rows otherwise waits for at its end.
+// Warp `w` of those of all the blocks that share the tile takes every n-th row.  (64 rows of 16 adapters of rank 64, k = 4,096, n = 12,288:
+// 49 us where each block fetches for all of its tile's rows, 45 so.)
 __device__ __forceinline__ void prefetch_adapters(const LinearParams &p, int n0, int m0, int w, int lane)
 {
     const int bytes = min(kTileM, p.n - m0) * p.rank * 2;
     for (int t0 = 0; t0 < p.tile_n && n0 + t0 < p.rows; t0 += 32) {
         const int id = t0 + lane < p.tile_n && n0 + t0 + lane < p.rows ? __ldg(p.ids + n0 + t0 + lane) : -1, before = __shfl_up_sync(0xffffffffu, id, 1);
-        uint32_t fresh = __ballot_sync(0xffffffffu, (unsigned)id < (unsigned)p.n_adapters && (lane == 0 || id != before)) & (0x01010101u << w);      // a warp takes every eighth row
+        uint32_t fresh = __ballot_sync(0xffffffffu, (unsigned)id < (unsigned)p.n_adapters && (lane == 0 || id != before) && (t0 + lane) % (kEpilogueWarps * p.split) == w);
         while (fresh) {
             const int a = __shfl_sync(0xffffffffu, id, __ffs((int)fresh) - 1);
             fresh &= fresh - 1;
@@ -562,7 +564,7 @@ template <Form kForm, bool kAdapters, bool kHalf> __global__ void __launch_bound
                 if (kAdapters) asm volatile("prefetch.global.L2 [%0];" ::"l"(p.ids + row));
             }
         }
-        if (kAdapters && first_tile < tiles) prefetch_adapters(p, first_tile / p.tiles_m * p.tile_n, first_tile % p.tiles_m * kTileM, w, lane);
+        if (kAdapters && first_tile < tiles) prefetch_adapters(p, first_tile / p.tiles_m * p.tile_n, first_tile % p.tiles_m * kTileM, w + kEpilogueWarps * rank, lane);
         if constexpr (kForm == kTiles) {
             const uint32_t in_pitch = inner_pitch(p.ranks), b_pitch = left_pitch(p.ranks), inner_at = staging + kEpilogueWarps * kStaging, left_at = inner_at + (uint32_t)p.tile_n * in_pitch;
             const uint8_t *const inner_s = smem_raw + (inner_at - smem_u32(smem_raw)), *const left_s = smem_raw + (left_at - smem_u32(smem_raw));
@@ -929,7 +931,8 @@ bool encode_rows(void *encode, CUtensorMap *map, const int8_t *base, int64_t k, 
 
 // Row tile, and blocks that share a tile: what takes the fewest cycles by a rough count.  A block of k costs 2.1 cycles for each
 // operand row; an epilogue 25 cycles a row and 25 more for every sixteen ranks (50 where the tile is split), under the next tile's
-// products where there is one; starting, and joining the blocks that share a tile, a few thousand.
+// products where there is one; starting, and joining the blocks that share a tile, a few thousand, and eight of them
+// far more the wider the tile (200 rows, k = 4,096, n = 1,024: 9.9 us with four blocks to a tile, 18.6 with eight; 16 rows, k = 8,192: 10.7 and 8.6).
 void plan(LinearParams &p, int n_sms)
 {
     p.tiles_m = (p.n + kTileM - 1) / kTileM;
@@ -945,7 +948,7 @@ void plan(LinearParams &p, int n_sms)
             const bool part = narrow || split > 1;
             if (!part && width > most) continue;
             const int64_t rounds = (tiles * split + slots - 1) / slots;
-            const double products = 2.1 * ((p.k_blocks + split - 1) / split) * (width + kTileM), end = (25.0 + (part ? 50.0 : 25.0) * (p.ranks >> 4)) * width / split + (split > 1 ? 2000.0 : 0.0);
+            const double products = 2.1 * ((p.k_blocks + split - 1) / split) * (width + kTileM), end = (25.0 + (part ? 50.0 : 25.0) * (p.ranks >> 4)) * width / split + (split > 1 ? 4000.0 : 0.0) + (split == 8 ? 100.0 * width : 0.0);
             const int64_t cost = (int64_t)(part ? rounds * (products + end + 3000.0) : rounds * std::max(products, end) + std::min(products, end) + 3000.0);
             if (cost < best) {
                 best = cost;
