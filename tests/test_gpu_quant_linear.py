@@ -192,3 +192,13 @@ def test_ids_without_adapters_are_too_large():
         ids = torch.arange(rows, dtype=torch.int32, device="cuda") % 2 - 1
         y, plain = isc.quant_linear(s["x"], s["x_scale"], s["w"], s["w_scale"], adapters=none, adapter_ids=ids), call(s)
         assert torch.equal(y[ids < 0], plain[ids < 0]) and torch.isnan(y[ids >= 0]).all()
+
+
+@pytest.mark.parametrize("rows,k,n,adapters,rank", [(16, 8192, 1024, 8, 16), (13, 8192, 1000, 40, 4), (48, 16384, 2000, 9, 20), (100, 32768, 300, 5, 64), (3, 65536, 70, 2, 128)])
+@pytest.mark.parametrize("order", ["mixed", "runs"])
+def test_long_sums_of_few_outputs(rows, k, n, adapters, rank, order):
+    """Where the most blocks share a tile, narrow and wide ones."""
+    s = problem(rows, k, n, adapters=adapters, rank=rank, order=order, bias=True)
+    check(call(s, out_dtype=torch.float32), s, torch.float32)
+    s["adapters"] = s["adapter_ids"] = None
+    check(call(s, out_dtype=torch.bfloat16), s, torch.bfloat16)
