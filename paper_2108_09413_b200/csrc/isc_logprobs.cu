@@ -49,7 +49,7 @@ struct LogProbParams {
     int64_t rows, ld;
     int vocab, top, cluster;
     float scale, scale2;                // scale2 = scale log2(e)
-    float limit;                        // logits below it in magnitude take the short way
+    float least, limit;                 // rows whose largest logit lies between them take the short way (set_range)
 };
 
 __device__ __forceinline__ float exp2_fast(float v)
@@ -175,7 +175,8 @@ template <typename T> struct Row {
 };
 
 // Masked logits as numbers that a product with zero leaves zero: minus infinity as the lowest finite number that the type's arithmetic
-// below can do without (kMasked), and whatever lies under it.
+// below can do without (kMasked), and whatever lies under it.  It stands for a mask only where its exponential is zero as well: below a largest
+// logit that set_range gives.
 template <typename T> struct Finite {
     static constexpr float kMasked = -1e30f;
     static __device__ __forceinline__ Chunk<T> of(Chunk<T> c) { return c; }
@@ -207,6 +208,16 @@ template <> struct Finite<float> {
         return c;
     }
 };
+
+// Whether there is a mask among fp16 logits, where it has to be known (set_range).
+__device__ __forceinline__ bool any_masked(const Chunk<__half> &e)
+{
+    uint32_t least = 0x7BFF7BFFu;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) asm("min.f16x2 %0, %0, %1;" : "+r"(least) : "r"(reinterpret_cast<const uint32_t *>(&e)[j]));
+    return (least & 0xFFFFu) == 0xFC00u || least >> 16 == 0xFC00u;
+}
+template <typename T> __device__ __forceinline__ bool any_masked(const Chunk<T> &) { return true; }
 
 template <typename T> __device__ __forceinline__ float largest(const Chunk<T> &e)
 {
@@ -248,7 +259,8 @@ struct Own {
         s = make_pair(all.s, 0.0f);
         u = make_pair(all.u, 0.0f);
     }
-    // Logits between -1e30 and 1e29, but for masks, and factors below 1e8: no difference leaves single precision's range.
+    // Logits between -1e30 and 1e29, but for masks, and factors below 1e8: no difference leaves single precision's range.  No masks, or
+    // m far enough above kMasked that nothing at or below it weighs anything.
     template <typename T> __device__ __forceinline__ void add_plain(const Chunk<T> &masked, Pair minus_m, Pair c2)
     {
         const Chunk<T> e = Finite<T>::of(masked);
@@ -275,7 +287,7 @@ struct Own {
         u = add2(u, make_pair(weighted, 0.0f));
     }
     // chunks first, first + stride, ...: `n` of them
-    template <typename T, int kN> __device__ __forceinline__ void add(const Chunk<T> (&e)[kN], int n, int first, int stride, float c, float limit)
+    template <typename T, int kN> __device__ __forceinline__ void add(const Chunk<T> (&e)[kN], int n, int first, int stride, float c, float least, float limit)
     {
         float most[kN], all = -INFINITY;
 #pragma unroll
@@ -291,7 +303,14 @@ struct Own {
                 if (most[i] == all) best = first + i * stride;
             if (all > m) rise(all, c);
         }
-        if (m > (sizeof(T) == 2 ? Finite<T>::kMasked : -limit) && fabsf(m) < limit) {
+        bool plain = m > least;
+        if (sizeof(T) == 2 && !plain) {
+            plain = true;
+#pragma unroll
+            for (int i = 0; i < kN; ++i)
+                if (i < n && any_masked(e[i])) plain = false;
+        }
+        if (plain && fabsf(m) < limit) {
             const Pair minus_m = make_pair(-m, -m), c2 = make_pair(c, c);
 #pragma unroll
             for (int i = 0; i < kN; ++i)
@@ -520,7 +539,7 @@ template <typename T> __global__ void __launch_bounds__(kThreads) k_log_probs(co
 #pragma unroll
         for (int a = 0; a < kAhead; ++a)
             if (i0 + a * stride < row.chunks) e[a] = row.load(i0 + a * stride);
-        own.add(e, (row.chunks - i0 + stride - 1) / stride, i0, stride, c, p.limit);
+        own.add(e, (row.chunks - i0 + stride - 1) / stride, i0, stride, c, p.least, p.limit);
     }
     bool bad;
     Sums all = join_all(sh, team, own, edge, c, bad);
@@ -580,7 +599,7 @@ template <typename T> __global__ void __launch_bounds__(32 * kRowWarps) k_log_pr
 #pragma unroll
         for (int a = 0; a < kAhead; ++a)
             if (i0 + a * 32 < row.chunks) e[a] = row.load(i0 + a * 32);
-        own.add(e, (row.chunks - i0 + 31) / 32, i0, 32, c, p.limit);
+        own.add(e, (row.chunks - i0 + 31) / 32, i0, 32, c, p.least, p.limit);
     }
     bool bad;
     const Sums all = join_all(sh, team, own, edge, c, bad);
@@ -655,8 +674,8 @@ template <typename T> __global__ void __launch_bounds__(kStreamThreads + 32, kSt
 #pragma unroll
                 for (int i = 0; i < kTogether; ++i) e[i] = *reinterpret_cast<const Chunk<T> *>(pieces + slot * kPieceBytes + 16 * ((i0 + i) * kStreamThreads + t));
                 const int here = left - i0 * kStreamThreads;
-                if (here > (kTogether - 1) * kStreamThreads) own.add(e, kTogether, from + i0 * kStreamThreads + t, kStreamThreads, c, p.limit);
-                else if (here > 0) own.add(e, (here + kStreamThreads - 1) / kStreamThreads, from + i0 * kStreamThreads + t, kStreamThreads, c, p.limit);
+                if (here > (kTogether - 1) * kStreamThreads) own.add(e, kTogether, from + i0 * kStreamThreads + t, kStreamThreads, c, p.least, p.limit);
+                else if (here > 0) own.add(e, (here + kStreamThreads - 1) / kStreamThreads, from + i0 * kStreamThreads + t, kStreamThreads, c, p.least, p.limit);
             }
             __syncwarp();
             if ((t & 31) == 0) tc::mbar_arrive(tc::smem_u32(&empty[slot]));
@@ -755,8 +774,20 @@ template <typename T, int kLanes, int kHeld> __global__ void __launch_bounds__(k
     }
 }
 
+// The range of largest logits for the short way: single precision holds all differences, and (kMasked - m) c, the exponent that a
+// mask gets there, is kFloorZ at most, so that its exponential is zero.  bf16's and fp32's kMasked is out of reach down to factors of
+// 1e-28, but fp16's is near: m has to be above -65,400 at a factor of 1, and no m around zero is far enough below one of 0.0016.  Chunks
+// without masks go the short way there too (4,096 x 131,072 fp16 at 0.001: 262 us, at 1 248; with masks 518).  int8 has no masks.
+template <typename T> void set_range(LogProbParams &p)
+{
+    p.limit = p.scale2 < 1e8f ? 1e29f : -1e29f;
+    p.least = -1e29f;
+    if (sizeof(T) > 1) p.least = std::max(p.least, (float)std::min((double)Finite<T>::kMasked - (double)kFloorZ / (double)p.scale2, 3e38));
+}
+
 template <typename T> cudaError_t launch_log_probs(const Device &dev, LogProbParams p, cudaStream_t st)
 {
+    set_range<T>(p);
     if (p.vocab <= 64) {
         const int lanes = p.vocab <= 16 ? 1 : 8;
         const int64_t per_block = kGroupThreads / lanes;
@@ -821,7 +852,6 @@ extern "C" int isc_log_probs(const void *logits, int64_t ld, int type, int64_t r
     p.rows = rows; p.ld = ld; p.vocab = (int)vocab; p.top = top; p.cluster = 1;
     p.scale = scale;
     p.scale2 = scale * 1.44269504088896f;
-    p.limit = p.scale2 < 1e8f ? 1e29f : 0.0f;
     const cudaStream_t st = (cudaStream_t)cuda_stream;
     e = type == ISC_BF16 ? launch_log_probs<__nv_bfloat16>(dev, p, st) : type == ISC_F16 ? launch_log_probs<__half>(dev, p, st) :
         type == ISC_F32 ? launch_log_probs<float>(dev, p, st) : launch_log_probs<int8_t>(dev, p, st);
