@@ -62,3 +62,22 @@ def test_result_does_not_depend_on_the_rows_alignment(vocab):
         # each is within its own roundings: see `check`
         assert max(results) - min(results) <= 2 * 360 * 2.0**-24 * (2 + 2 * max(results))
 
+
+
+@pytest.mark.parametrize("vocab", [700, 20000, 131072])
+@pytest.mark.parametrize("scale", [1e-5, 1e-3, 1.0])
+def test_stretches_with_and_without_masks(vocab, scale):
+    """fp16's lowest number is no mask, beside masks and far from them."""
+    g = torch.Generator(device="cuda").manual_seed(vocab)
+    x = torch.randn(8, vocab + 1, device="cuda", generator=g) * 3.0
+    i = torch.arange(vocab + 1, device="cuda")
+    x[:, i // 64 % 3 == 1] = -65504.0
+    x[:, i // 100 % 4 == 2] = -math.inf
+    x[4:, i % 7 == 3] = -65504.0
+    x[6:] -= 65000.0
+    x[6:].clamp_(min=-65504.0)
+    x[6:, i // 200 % 2 == 0] = -math.inf
+    x = x.half()[:, :vocab]
+    check(x, some_targets(8, vocab, g), 5, scale)
+    many = x.repeat(120, 1)
+    check(many, some_targets(960, vocab, g), 5, scale)
