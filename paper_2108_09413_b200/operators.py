@@ -1,9 +1,10 @@
 """The library's operators on device tensors (the last part of include/isc.h) for torch tensors.
 
 Every call checks its arguments, allocates its outputs and enqueues one of the library's operators on `stream` (a torch
-stream; the current one of the tensors' device by default).  Outputs belong to that stream; inputs may be dropped after the
-call, whichever stream they belong to.  The operators compute no gradients: inputs that require one are refused while
-gradients are enabled.
+stream; the current one of the tensors' device by default).  Outputs belong to that stream.  Inputs may be dropped after a
+call on a side stream, whichever stream they belong to; on a device's default stream, as with torch's own operators, those
+of a side stream need `record_stream` first.  The operators compute no gradients: inputs that require one are refused
+while gradients are enabled.
 """
 from __future__ import annotations
 
@@ -72,21 +73,26 @@ def _empty(shape, dtype, device):
 
 
 def _enqueue(what, device, stream, call, tensors=()):
-    """`call(raw stream)`, a status, with the tensors' device and `stream` current.  The memory of `tensors` (or None), which may be
-    another stream's, is not given to others before `stream` has used it."""
+    """`call(raw stream)`, a status, with the tensors' device and `stream` (None: the current one) current.  The memory of `tensors`
+    (or None), which may be another stream's, is not given to others before a `stream` that was given, or is not the default one, has
+    used it."""
     torch = _torch
     index = device.index
     if stream is not None and stream.device_index != index:
         _refuse(what, "the stream belongs to another device than the tensors")
     if stream is None and index == torch.cuda.current_device():
-        rc = call(torch._C._cuda_getCurrentRawStream(index))
+        raw = torch._C._cuda_getCurrentRawStream(index)
+        rc = call(raw)
     else:
         with torch.cuda.device(index), torch.cuda.stream(stream if stream is not None else torch.cuda.current_stream(index)):
-            rc = call(torch._C._cuda_getCurrentRawStream(index))
-        if stream is not None:
-            for t in tensors:
-                if t is not None and t.numel():
-                    t.record_stream(stream)
+            raw = torch._C._cuda_getCurrentRawStream(index)
+            rc = call(raw)
+    if raw or stream is not None:
+        if stream is None:
+            stream = torch.cuda.current_stream(index)
+        for t in tensors:
+            if t is not None and t.numel():
+                t.record_stream(stream)
     if rc != 0:
         raise IscError(rc, what)
 
