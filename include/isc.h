@@ -453,8 +453,10 @@ int isc_log_probs(const void *logits, int64_t ld, int type, int64_t rows, int64_
                   float *out_top_log_probs, int32_t *votes, void *cuda_stream);
 
 /*
- * isc_operator_status -- waits for `cuda_stream` and tells whether a bounded wait of an operator's kernel has run out on the
- * current device since the last call (its rows' scales or results are NaN then).  Not to be captured.
+ * isc_operator_status -- waits for `cuda_stream` and tells the calling thread whether a bounded wait of an operator's kernel has
+ * run out on the current device, on whatever stream, since the thread's last call (its first call: since the library was
+ * loaded); the rows' scales or results are NaN then.  What one thread is told is not taken away from another.  Not to be
+ * captured.
  * Returns ISC_OK, ISC_ERR_TIMEOUT, or ISC_ERR_CUDA when the stream's work failed.
  */
 int isc_operator_status(void *cuda_stream);

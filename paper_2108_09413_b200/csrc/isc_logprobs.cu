@@ -39,7 +39,7 @@ constexpr int kMostCluster = 8;
 constexpr float kFloorZ = -150.0f;      // exp2 of it is zero in single precision
 typedef unsigned long long Key;
 
-__device__ int timeout_word;            // not zero: a bounded wait has run out
+__device__ uint32_t timeouts;            // bounded waits that have run out
 
 struct LogProbParams {
     const void *logits;
@@ -632,7 +632,7 @@ template <typename T> __global__ void __launch_bounds__(kStreamThreads + 32, kSt
             for (int64_t r = blockIdx.x; r < p.rows && !failed; r += gridDim.x) {
                 const Row<T> row(logits + r * p.ld, p.vocab);
                 for (int from = 0; from < row.chunks; from += kPieceChunks) {
-                    if (use && !wait_limited(tc::smem_u32(&empty[slot]), (uint32_t)(use - 1) & 1u, &failed)) { timeout_word = 1; break; }
+                    if (use && !wait_limited(tc::smem_u32(&empty[slot]), (uint32_t)(use - 1) & 1u, &failed)) { count_timeout(&timeouts); break; }
                     const uint32_t bytes = 16u * (uint32_t)min(kPieceChunks, row.chunks - from), bar = tc::smem_u32(&full[slot]);
                     tc::mbar_expect_tx(bar, bytes);
                     tc::bulk_g2s(tc::smem_u32(pieces + slot * kPieceBytes), reinterpret_cast<const uint8_t *>(row.body()) + 16 * (int64_t)from, bytes, bar);
@@ -664,7 +664,7 @@ template <typename T> __global__ void __launch_bounds__(kStreamThreads + 32, kSt
         int left_in_subset = per_subset, at_subset = t;
         sh.candidate[t + kStreamThreads] = 0;
         for (int from = 0; from < row.chunks; from += kPieceChunks) {
-            if (!wait_limited(tc::smem_u32(&full[slot]), (uint32_t)use & 1u, &failed)) { timeout_word = 1; own.seen = NAN; }
+            if (!wait_limited(tc::smem_u32(&full[slot]), (uint32_t)use & 1u, &failed)) { count_timeout(&timeouts); own.seen = NAN; }
             const int left = row.chunks - from - t;
             // (int8: one chunk has 16 logits, and there are no registers for more)
             constexpr int kN = kPieceChunks / kStreamThreads, kTogether = sizeof(T) == 1 ? 1 : kN;
@@ -828,7 +828,7 @@ template <typename T> cudaError_t launch_log_probs(const Device &dev, LogProbPar
 }  // namespace
 
 namespace ops {
-cudaError_t log_probs_take_timeout(cudaStream_t st, bool *expired) { return take_timeout(timeout_word, st, expired); }
+cudaError_t log_probs_timeouts(cudaStream_t st, uint32_t *count) { return read_timeouts(timeouts, st, count); }
 }  // namespace ops
 }  // namespace isc
 

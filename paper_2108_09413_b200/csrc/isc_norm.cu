@@ -34,7 +34,7 @@ namespace {
 
 using namespace ops;
 
-__device__ int timeout_word;            // not zero: a bounded wait has run out
+__device__ uint32_t timeouts;            // bounded waits that have run out
 
 constexpr int kChunks = 2;              // chunks of eight elements a thread holds
 constexpr int kBlock = 1024;            // most threads for a row
@@ -501,7 +501,7 @@ template <typename T, typename W> __global__ void __launch_bounds__(kRingThreads
     }
     int slot = 0, use = 0;
     for (int64_t row = first; row < p.rows; row += stride) {
-        if (!wait_limited(tc::smem_u32(&full[which][slot]), (uint32_t)use & 1u, &failed)) timeout_word = 1;
+        if (!wait_limited(tc::smem_u32(&full[which][slot]), (uint32_t)use & 1u, &failed)) count_timeout(&timeouts);
         const T *xs = reinterpret_cast<const T *>(mine + slot * slot_bytes), *rs = reinterpret_cast<const T *>(mine + slot * slot_bytes + row_bytes);
         Partial part;
         Pair prod[kN][4];
@@ -591,7 +591,7 @@ template <typename T> cudaError_t launch_norm(const Device &dev, const NormParam
 }  // namespace
 
 namespace ops {
-cudaError_t norm_take_timeout(cudaStream_t st, bool *expired) { return take_timeout(timeout_word, st, expired); }
+cudaError_t norm_timeouts(cudaStream_t st, uint32_t *count) { return read_timeouts(timeouts, st, count); }
 }  // namespace ops
 }  // namespace isc
 

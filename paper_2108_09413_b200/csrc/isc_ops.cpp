@@ -10,14 +10,13 @@ namespace ops {
 
 cudaError_t current_device(Device *out)
 {
-    constexpr int kMost = 64;
-    static std::atomic<int> sms[kMost];
-    static std::atomic<void *> encoder[kMost];
+    static std::atomic<int> sms[kMostDevices];
+    static std::atomic<void *> encoder[kMostDevices];
     int ordinal = 0;
     cudaError_t e = cudaGetDevice(&ordinal);
     if (e != cudaSuccess) return e;
-    const int slot = ordinal < kMost ? ordinal : kMost - 1;
-    int n = ordinal < kMost ? sms[slot].load(std::memory_order_acquire) : 0;
+    const int slot = ordinal < kMostDevices ? ordinal : kMostDevices - 1;
+    int n = ordinal < kMostDevices ? sms[slot].load(std::memory_order_acquire) : 0;
     void *fn = encoder[slot].load(std::memory_order_acquire);
     if (!n) {
         e = cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, ordinal);
@@ -28,7 +27,7 @@ cudaError_t current_device(Device *out)
             cudaGetLastError();
         }
         encoder[slot].store(fn, std::memory_order_release);
-        if (ordinal < kMost) sms[slot].store(n, std::memory_order_release);
+        if (ordinal < kMostDevices) sms[slot].store(n, std::memory_order_release);
     }
     *out = Device{ordinal, n, fn};
     return cudaSuccess;
@@ -48,10 +47,21 @@ int status_of(cudaError_t e, const char *what)
 extern "C" int isc_operator_status(void *cuda_stream)
 {
     using namespace isc::ops;
-    bool norm = false, linear = false, log_probs = false;
-    cudaError_t e = norm_take_timeout((cudaStream_t)cuda_stream, &norm);
-    if (e == cudaSuccess) e = linear_take_timeout((cudaStream_t)cuda_stream, &linear);
-    if (e == cudaSuccess) e = log_probs_take_timeout((cudaStream_t)cuda_stream, &log_probs);
+    // what this thread has been told of: another thread's question takes nothing away from it
+    static thread_local uint32_t told[kMostDevices][3];
+    const cudaStream_t st = (cudaStream_t)cuda_stream;
+    int ordinal = 0;
+    uint32_t now[3] = {};
+    cudaError_t e = cudaGetDevice(&ordinal);
+    if (e == cudaSuccess) e = norm_timeouts(st, &now[0]);
+    if (e == cudaSuccess) e = linear_timeouts(st, &now[1]);
+    if (e == cudaSuccess) e = log_probs_timeouts(st, &now[2]);
     if (e != cudaSuccess) return status_of(e, "operator_status");
-    return norm || linear || log_probs ? ISC_ERR_TIMEOUT : ISC_OK;
+    uint32_t *const mine = told[ordinal < kMostDevices ? ordinal : kMostDevices - 1];
+    bool more = false;
+    for (int i = 0; i < 3; ++i) {
+        more |= now[i] != mine[i];
+        mine[i] = now[i];
+    }
+    return more ? ISC_ERR_TIMEOUT : ISC_OK;
 }

@@ -34,19 +34,13 @@ template <> __device__ __forceinline__ float from_float<float>(float v) { return
 template <> __device__ __forceinline__ __half from_float<__half>(float v) { return __float2half_rn(v); }
 template <> __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
 
-// Reads a kernel file's timeout word after `st`'s work, and clears it.
-template <typename Word> cudaError_t take_timeout(const Word &device_word, cudaStream_t st, bool *expired)
+// A kernel file's number of bounded waits that have run out.  It only grows, so that no reader takes it away from another.
+__device__ __forceinline__ void count_timeout(uint32_t *timeouts) { atomicAdd(timeouts, 1u); }
+// The number after `st`'s work.
+inline cudaError_t read_timeouts(const uint32_t &timeouts, cudaStream_t st, uint32_t *count)
 {
-    int word = 0;
-    cudaError_t e = cudaMemcpyFromSymbolAsync(&word, device_word, sizeof(word), 0, cudaMemcpyDeviceToHost, st);
-    if (e == cudaSuccess) e = cudaStreamSynchronize(st);
-    *expired = word != 0;
-    if (e == cudaSuccess && word) {
-        word = 0;
-        e = cudaMemcpyToSymbolAsync(device_word, &word, sizeof(word), 0, cudaMemcpyHostToDevice, st);
-        if (e == cudaSuccess) e = cudaStreamSynchronize(st);
-    }
-    return e;
+    const cudaError_t e = cudaMemcpyFromSymbolAsync(count, timeouts, sizeof(*count), 0, cudaMemcpyDeviceToHost, st);
+    return e == cudaSuccess ? cudaStreamSynchronize(st) : e;
 }
 
 // Eight elements as they lie in memory.

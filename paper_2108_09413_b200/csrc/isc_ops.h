@@ -15,16 +15,17 @@ inline bool aligned(const void *p, size_t to) { return ((uintptr_t)p & (to - 1))
 
 // The current device as the operators' launches need it.  Filled once per device; a second thread that comes meanwhile fills it
 // with the same values.
+constexpr int kMostDevices = 64;          // whose properties are kept
 struct Device {
     int ordinal, n_sms;
     void *encode;             // the driver's cuTensorMapEncodeTiled, or null
 };
 cudaError_t current_device(Device *out);
 
-// Whether a bounded wait of the operators' kernels has run out on the current device since the last call; waits for `st`.
-cudaError_t norm_take_timeout(cudaStream_t st, bool *expired);
-cudaError_t linear_take_timeout(cudaStream_t st, bool *expired);
-cudaError_t log_probs_take_timeout(cudaStream_t st, bool *expired);
+// How many bounded waits of the operators' kernels have run out on the current device; wait for `st`.
+cudaError_t norm_timeouts(cudaStream_t st, uint32_t *count);
+cudaError_t linear_timeouts(cudaStream_t st, uint32_t *count);
+cudaError_t log_probs_timeouts(cudaStream_t st, uint32_t *count);
 
 // A failed CUDA call as a status; clears the runtime's sticky copy of the error.
 int status_of(cudaError_t e, const char *what);

@@ -48,7 +48,7 @@ namespace {
 using namespace ops;
 using namespace tc;
 
-__device__ int timeout_word;            // not zero: a bounded wait has run out
+__device__ uint32_t timeouts;            // bounded waits that have run out
 
 constexpr int kTileM = 128, kBlockK = 128;
 constexpr int kEpilogueWarps = 8, kThreads = 32 * (2 + kEpilogueWarps);
@@ -505,7 +505,7 @@ template <Form kForm, bool kAdapters, bool kHalf> __global__ void __launch_bound
             for (int tile = first_tile; tile < tiles && !failed; tile += tile_step) {
                 const int m0 = tile % p.tiles_m * kTileM, n0 = tile / p.tiles_m * p.tile_n;
                 for (int kb = kb0; kb < kb1; ++kb) {
-                    if (use && !wait_limited(smem_u32(&bar_free[s]), (uint32_t)(use - 1) & 1u, &failed)) { timeout_word = 1; break; }
+                    if (use && !wait_limited(smem_u32(&bar_free[s]), (uint32_t)(use - 1) & 1u, &failed)) { count_timeout(&timeouts); break; }
                     const uint32_t bar = smem_u32(&bar_full[s]), at = ring + (uint32_t)s * stage_bytes;
                     mbar_expect_tx(bar, (uint32_t)(kTileM + p.tile_n) * kBlockK);
                     copy_tile(at, &p.map_w, kb * kBlockK, m0, bar);
@@ -528,10 +528,10 @@ template <Form kForm, bool kAdapters, bool kHalf> __global__ void __launch_bound
             int s = 0, use = 0, j = 0;
             for (int tile = first_tile; tile < tiles && !failed; tile += tile_step, ++j) {
                 const int buf = j & 1;
-                if (j >= 2 && !wait_limited(smem_u32(&bar_acc_free[buf]), (uint32_t)((j >> 1) - 1) & 1u, &failed)) { timeout_word = 1; break; }
+                if (j >= 2 && !wait_limited(smem_u32(&bar_acc_free[buf]), (uint32_t)((j >> 1) - 1) & 1u, &failed)) { count_timeout(&timeouts); break; }
                 tc_fence_after();
                 for (int kb = kb0; kb < kb1; ++kb) {
-                    if (!wait_limited(smem_u32(&bar_full[s]), (uint32_t)use & 1u, &failed)) { timeout_word = 1; break; }
+                    if (!wait_limited(smem_u32(&bar_full[s]), (uint32_t)use & 1u, &failed)) { count_timeout(&timeouts); break; }
                     tc_fence_after();
                     const uint64_t a = operand(ring + (uint32_t)s * stage_bytes), b = operand(ring + (uint32_t)s * stage_bytes + kTileM * kBlockK);
 #pragma unroll
@@ -600,7 +600,7 @@ template <Form kForm, bool kAdapters, bool kHalf> __global__ void __launch_bound
                 }
                 const bool ok = __all_sync(0xffffffffu, wait_limited(smem_u32(&bar_acc_full[buf]), (uint32_t)(j >> 1) & 1u, &failed)) != 0;
                 if (!ok) {              // nothing of the tile can be told
-                    timeout_word = 1;
+                    count_timeout(&timeouts);
 #pragma unroll
                     for (int i = 0; i < 4; ++i) strip.w_scale[i] = strip.bias[i] = NAN;
                 }
@@ -656,7 +656,7 @@ template <Form kForm, bool kAdapters, bool kHalf> __global__ void __launch_bound
             }
             // this block's sums to its shared memory; its ring is empty: all products are done
             const bool ok = __all_sync(0xffffffffu, wait_limited(smem_u32(&bar_acc_full[0]), 0, &failed)) != 0;
-            if (!ok) timeout_word = 1;
+            if (!ok) count_timeout(&timeouts);
             tc_fence_after();
             for (int q = half; q < p.tile_n / 16; q += 2) {
                 int v[16];
@@ -1005,7 +1005,7 @@ cudaError_t launch_inner(InnerParams p, int type, int n_sms, cudaStream_t st)
 }  // namespace
 
 namespace ops {
-cudaError_t linear_take_timeout(cudaStream_t st, bool *expired) { return take_timeout(timeout_word, st, expired); }
+cudaError_t linear_timeouts(cudaStream_t st, uint32_t *count) { return read_timeouts(timeouts, st, count); }
 }  // namespace ops
 }  // namespace isc
 
