@@ -4,7 +4,7 @@ Every call checks its arguments, allocates its outputs and enqueues one of the l
 stream; the current one of the tensors' device by default).  Outputs belong to that stream.  Inputs may be dropped after a
 call on a side stream, whichever stream they belong to; on a device's default stream, as with torch's own operators, those
 of a side stream need `record_stream` first.  The operators compute no gradients: inputs that require one are refused
-while gradients are enabled.
+while gradients are enabled, and inputs with a tangent (forward-mode differentiation) always.
 """
 from __future__ import annotations
 
@@ -30,8 +30,10 @@ def _refuse(what, why):
 
 
 def _same_device(what, tensors):
-    """The one GPU that all of the tensors (or None) are on; none of them may need a gradient."""
+    """The one GPU that all of the tensors (or None) are on; none of them may need a gradient or have a tangent."""
     torch = _torch
+    forward = torch.autograd.forward_ad
+    dual = forward._current_level >= 0
     first = tensors[0]
     if not isinstance(first, torch.Tensor) or not first.is_cuda:
         _refuse(what, "tensors have to be on a GPU")
@@ -40,7 +42,7 @@ def _same_device(what, tensors):
         if t is not None:
             if not isinstance(t, torch.Tensor) or t.device != device:
                 _refuse(what, "tensors have to be on one GPU")
-            if grad and t.requires_grad:
+            if grad and t.requires_grad or dual and forward.unpack_dual(t).tangent is not None:
                 _refuse(what, "no gradients are computed")
     return device
 
