@@ -20,8 +20,8 @@ _types = {}
 def _start():
     global _torch
     import torch
-    _torch = torch
     _types.update({torch.bfloat16: 0, torch.float16: 1, torch.float32: 2, torch.int8: 3})
+    _torch = torch            # last: another thread that finds it set looks into _types
     return torch
 
 
