@@ -616,7 +616,7 @@ extern "C" int isc_rms_norm_quant(const void *x, int64_t ldx, const void *residu
     const auto wide = [&](const void *a, int64_t ld) { return aligned(a, 16) && (rows == 1 || ld * bytes % 16 == 0); };
     p.vec = wide(x, ldx) && (!residual || wide(residual, ldr));
     p.vec_w = aligned(weight, 16);
-    p.vec_h = wide(sum, lds);
+    p.vec_h = !sum || wide(sum, lds);
     p.vec_q = aligned(q, 8) && (rows == 1 || ldq % 8 == 0);
     const cudaStream_t st = (cudaStream_t)cuda_stream;
     Device dev;

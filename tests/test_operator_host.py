@@ -70,7 +70,25 @@ def every_thread_is_told_of_a_timeout():
     assert _in_a_thread(status) == TIMEOUT              # a thread's first: since the library was loaded
 
 
-TESTS = [every_thread_is_told_of_a_timeout]
+AT = 0x10000                                  # an aligned address nobody owns
+
+
+def a_sum_s_pitch_counts_only_with_a_sum():
+    """Which form of the norm runs does not depend on what a caller who wants no sum passes as its pitch."""
+    import paper_2108_09413_b200 as isc
+    f = _fake()
+
+    def kernel(total, lds, rows=20000, width=4096):
+        f.fake_reset()
+        assert isc.lib().isc_rms_norm_quant(AT, width, AT, width, AT, 0, 0, rows, width, 1e-6, total, lds, AT, width, AT, None) == OK
+        assert f.fake_launches() == 1
+        return next(n for n in ("k_norm_ring", "k_norm_block") if n in f.fake_launch_name(0).decode())
+    for lds in (0, 1, 4095, 4097, -1, 2**40 + 1):
+        assert kernel(None, lds) == "k_norm_ring", lds
+    assert kernel(AT, 4096) == "k_norm_ring" and kernel(AT, 4097) == "k_norm_block"
+
+
+TESTS = [every_thread_is_told_of_a_timeout, a_sum_s_pitch_counts_only_with_a_sum]
 
 
 @pytest.mark.parametrize("test", [t.__name__ for t in TESTS])
