@@ -9,7 +9,7 @@
 // 7 2^-24 |v|; where v is nearer than 10 2^-24 |v| to the middle between two codes (the three units between them cover the test's own
 // roundings), p and max |p| are computed in double precision, from the row as it lies in memory, and divided there.  Of 8,192 plain Gaussian
 // bf16 elements one row in five has such a code, of a residual stream with a few large channels one in fifty.  Rows whose sums
-// leave the range of single precision (values above 1e19 or all below 1e-15, zeros, infinities, NaN) are computed in double
+// leave the range of single precision (values above 1e18, products above 1e20, all of either tiny, zeros, infinities, NaN) are computed in double
 // precision altogether.
 //
 // Forms.  Many rows of more than 1,024 16-bit (512 32-bit) elements: persistent blocks whose teams bring rows ahead by bulk copies (k_norm_ring).
@@ -48,7 +48,7 @@ struct NormParams {
     float *scale;
     int64_t rows, ldx, ldr, ldh, ldq;
     int width;
-    float eps;
+    float eps, most_ss;                 // most_ss: largest sum of squares that single precision settles
     bool wide_w;                        // weights in single precision beside narrower rows
     bool vec, vec_w, vec_h, vec_q;      // 16-byte accesses (8-byte for q) are aligned
 };
@@ -101,8 +101,9 @@ template <typename T> __device__ __forceinline__ void fetch_weights(const NormPa
 template <typename T> __device__ __forceinline__ double exact_sum(T x, T r, bool has_r) { return has_r ? (double)to_float(x) + (double)to_float(r) : (double)to_float(x); }
 
 // Where single precision leaves no doubt about anything but codes next to the middle between two: the range in which the sums
-// keep their relative error.
-__device__ __forceinline__ bool in_range(Sums s) { return s.ss >= 1e-30f && s.ss <= 1e37f && s.most >= 1e-30f && s.most <= 1e37f; }
+// keep their relative error, and in which nothing on the way to the scale leaves it: a largest product of 1e20 over a root of 1e-15 / 128 is
+// a number still, and a mean square added to eps is one (most_ss).
+__device__ __forceinline__ bool in_range(Sums s, float most_ss) { return s.ss >= 1e-30f && s.ss <= most_ss && s.most >= 1e-30f && s.most <= 1e20f; }
 // 127 / most; the reciprocal is within one unit in the last place
 __device__ __forceinline__ float step_inverse(float most)
 {
@@ -331,7 +332,7 @@ __device__ __forceinline__ void norm_row(const NormParams &p, int64_t row, const
         }
     }
     const Sums s = team.total(part.sums());
-    const bool plain = in_range(s);
+    const bool plain = in_range(s, p.most_ss);
     const float inv = step_inverse(s.most);
     uint2 code[kChunks];
     float doubt = plain ? 0.0f : 1.0f, scale = t == 0 ? row_scale(s, p.width, p.eps) : 0.0f;
@@ -520,7 +521,7 @@ template <typename T, typename W> __global__ void __launch_bounds__(kRingThreads
             if (p.h) store_eight(static_cast<T *>(p.h) + row * p.ldh + base[c], e);
         }
         const Sums s = team.total(part.sums());
-        const bool plain = in_range(s);
+        const bool plain = in_range(s, p.most_ss);
         const float inv = step_inverse(s.most);
         uint2 code[kN];
         float doubt = plain ? 0.0f : 1.0f, scale = t == 0 ? row_scale(s, p.width, p.eps) : 0.0f;
@@ -612,6 +613,7 @@ extern "C" int isc_rms_norm_quant(const void *x, int64_t ldx, const void *residu
     p.rows = rows; p.ldx = ldx; p.ldr = ldr; p.ldh = lds; p.ldq = ldq;
     p.width = (int)width;
     p.eps = eps;
+    p.most_ss = eps <= 1e38f ? 1e37f : 0.0f;      // (beyond, no row: a sum with eps may not be a number)
     p.wide_w = weight_type == ISC_F32 && type != ISC_F32;
     const auto wide = [&](const void *a, int64_t ld) { return aligned(a, 16) && (rows == 1 || ld * bytes % 16 == 0); };
     p.vec = wide(x, ldx) && (!residual || wide(residual, ldr));
