@@ -1049,24 +1049,28 @@ extern "C" int isc_quant_linear(const int8_t *x, int64_t ldx, const float *x_sca
     const cudaStream_t st = (cudaStream_t)cuda_stream;
     const bool half = ad && ad->type == ISC_F16;
     if (ad) {
+        p.b = ad->b; p.ids = ad->ids; p.inner = static_cast<float *>(work);
+        p.rank = ad->rank; p.ranks = (ad->rank + 15) & ~15; p.n_adapters = ad->n_adapters;
+    }
+    if (rows > 1) {                     // (before anything is launched: it may refuse)
+        plan(p, dev.n_sms);
+        if ((int64_t)p.tiles_m * p.tiles_n > INT32_MAX / kMostSplit) return ISC_ERR_UNSUPPORTED;
+    }
+    if (ad) {
         InnerParams q = {};
         q.x = x; q.a = ad->a; q.scale = ad->scale; q.ids = ad->ids;
         q.inner = static_cast<float *>(work);
-        q.ranks = p.ranks = (ad->rank + 15) & ~15;
+        q.ranks = p.ranks;
         q.ldx = ldx; q.rows = (int)rows; q.k = (int)k; q.rank = ad->rank; q.n_adapters = ad->n_adapters;
         q.vec_a = k % 8 == 0;
         e = launch_inner(q, ad->type, dev.n_sms, st);
         if (e != cudaSuccess) return status_of(e, "quant_linear, inner sums");
-        p.b = ad->b; p.ids = ad->ids; p.inner = q.inner;
-        p.rank = ad->rank; p.n_adapters = ad->n_adapters;
     }
     if (rows == 1) {
         const OneParams one = {x, w, x_scale, w_scale, bias, p.inner, p.b, p.ids, y, ldw, p.n, (int)k, p.rank, p.n_adapters, y_type};
         e = launch(half ? k_quant_linear_one<true> : k_quant_linear_one<false>, one, dim3((unsigned)((n + kOneThreads / 32 - 1) / (kOneThreads / 32))), kOneThreads, 0, 1, ad != nullptr, st);
         return status_of(e, "quant_linear");
     }
-    plan(p, dev.n_sms);
-    if ((int64_t)p.tiles_m * p.tiles_n > INT32_MAX / kMostSplit) return ISC_ERR_UNSUPPORTED;
     if (!dev.encode || !encode_rows(dev.encode, &p.map_w, w, k, n, ldw, kTileM) || !encode_rows(dev.encode, &p.map_x, x, k, rows, ldx, p.tile_n)) return ISC_ERR_CUDA;
     void (*const kernel)(LinearParams) =
         p.form == kPart ? (!ad ? k_quant_linear<kPart, false, false> : half ? k_quant_linear<kPart, true, true> : k_quant_linear<kPart, true, false>) :

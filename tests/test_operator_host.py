@@ -88,7 +88,24 @@ def a_sum_s_pitch_counts_only_with_a_sum():
     assert kernel(AT, 4096) == "k_norm_ring" and kernel(AT, 4097) == "k_norm_block"
 
 
-TESTS = [every_thread_is_told_of_a_timeout, a_sum_s_pitch_counts_only_with_a_sum]
+def nothing_is_launched_for_a_refused_projection():
+    """A projection of more tiles than are supported is refused as a whole: the adapters' inner sums are not computed either."""
+    import paper_2108_09413_b200 as isc
+    from paper_2108_09413_b200.operators import _Adapters
+    f, lib = _fake(), isc.lib()
+    parts = _Adapters(AT, AT, AT, AT, 0, 4, 16)
+
+    def call(rows, n):
+        f.fake_reset()
+        size = C.c_int64()
+        assert lib.isc_quant_linear_work_space(rows, 16, C.byref(size)) == OK
+        return lib.isc_quant_linear(AT, 64, AT, rows, AT, 64, AT, 64, n, None, C.addressof(parts), AT, n, 0, AT, size.value, None), f.fake_launches()
+    assert call(2**29, 2**29) == (-3, 0)
+    assert call(2**20, 2**30 - 2) == (-3, 0)
+    assert call(300, 1000) == (OK, 2) and call(1, 1000) == (OK, 2)
+
+
+TESTS = [every_thread_is_told_of_a_timeout, a_sum_s_pitch_counts_only_with_a_sum, nothing_is_launched_for_a_refused_projection]
 
 
 @pytest.mark.parametrize("test", [t.__name__ for t in TESTS])
