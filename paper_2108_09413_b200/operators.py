@@ -29,8 +29,9 @@ def _refuse(what, why):
     raise IscError(_ARG, f"{what}: {why}")
 
 
-def _same_device(what, tensors):
-    """The one GPU that all of the tensors (or None) are on; none of them may need a gradient or have a tangent."""
+def _same_device(what, tensors, needed=1):
+    """The one GPU that all of the tensors are on (None behind the first `needed` of them: not given); none may need a gradient or have a
+    tangent."""
     torch = _torch
     forward = torch.autograd.forward_ad
     dual = forward._current_level >= 0
@@ -39,11 +40,15 @@ def _same_device(what, tensors):
         _refuse(what, "tensors have to be on a GPU")
     device, grad = first.device, torch.is_grad_enabled()
     for t in tensors:
-        if t is not None:
+        if t is None:
+            if needed > 0:
+                _refuse(what, "a tensor is missing")
+        else:
             if not isinstance(t, torch.Tensor) or t.device != device:
                 _refuse(what, "tensors have to be on one GPU")
             if grad and t.requires_grad or dual and forward.unpack_dual(t).tangent is not None:
                 _refuse(what, "no gradients are computed")
+        needed -= 1
     return device
 
 
@@ -110,7 +115,7 @@ def rms_norm_quant(x, weight, eps=1e-6, residual=None, sum_out=None, stream=None
     torch = _torch or _start()
     what = "rms_norm_quant"
     given = (x, weight, residual, sum_out)
-    device = _same_device(what, given)
+    device = _same_device(what, given, 2)
     dtype, shape = x.dtype, x.shape
     code = _types.get(dtype, 3)
     if code == 3:
@@ -152,9 +157,14 @@ def quant_linear(x, x_scale, w, w_scale, bias=None, adapters=None, adapter_ids=N
     """
     torch = _torch or _start()
     what = "quant_linear"
-    a, b, factor = adapters if adapters is not None else (None, None, None)
+    a = b = factor = None
+    if adapters is not None:
+        adapters = tuple(adapters)
+        if len(adapters) != 3 or any(t is None for t in adapters):
+            _refuse(what, "adapters are three tensors")
+        a, b, factor = adapters
     given = (x, x_scale, w, w_scale, bias, a, b, factor, adapter_ids, out)
-    device = _same_device(what, given)
+    device = _same_device(what, given, 4)
     ldx, ldw = _pitch(what, "x", x, torch.int8), _pitch(what, "w", w, torch.int8)
     rows, k = x.shape
     n = w.shape[0]
@@ -219,6 +229,8 @@ def log_probs(logits, targets=None, top=0, scale=1.0, votes=None, entropy=True, 
         _refuse(what, "logits have to be bfloat16, float16, float32 or int8")
     ld = _pitch(what, "logits", logits)
     rows, vocab = logits.shape
+    if not 0 <= top <= 32:
+        _refuse(what, "top is 0 to 32")
     _vector(what, "targets", targets, torch.int64, rows)
     _vector(what, "votes", votes, torch.int32, vocab)
     given = h = ids = alternatives = None
