@@ -13,13 +13,14 @@ import ctypes as C
 from .binding import IscError, lib
 
 _ARG = -1
-_torch = None                 # imported with the first call: the rest of the package works without it
+_torch = _forward = None      # imported with the first call: the rest of the package works without them
 _types = {}
 
 
 def _start():
-    global _torch
+    global _torch, _forward
     import torch
+    from torch.autograd import forward_ad as _forward
     _types.update({torch.bfloat16: 0, torch.float16: 1, torch.float32: 2, torch.int8: 3})
     _torch = torch            # last: another thread that finds it set looks into _types
     return torch
@@ -29,26 +30,19 @@ def _refuse(what, why):
     raise IscError(_ARG, f"{what}: {why}")
 
 
-def _same_device(what, tensors, needed=1):
-    """The one GPU that all of the tensors are on (None behind the first `needed` of them: not given); none may need a gradient or have a
-    tangent."""
+def _same_device(what, tensors):
+    """The one GPU that all of the tensors (or None) are on; none of them may need a gradient or have a tangent."""
     torch = _torch
-    forward = torch.autograd.forward_ad
-    dual = forward._current_level >= 0
     first = tensors[0]
     if not isinstance(first, torch.Tensor) or not first.is_cuda:
         _refuse(what, "tensors have to be on a GPU")
-    device, grad = first.device, torch.is_grad_enabled()
+    device, grad, dual = first.device, torch.is_grad_enabled(), _forward._current_level >= 0
     for t in tensors:
-        if t is None:
-            if needed > 0:
-                _refuse(what, "a tensor is missing")
-        else:
+        if t is not None:
             if not isinstance(t, torch.Tensor) or t.device != device:
                 _refuse(what, "tensors have to be on one GPU")
-            if grad and t.requires_grad or dual and forward.unpack_dual(t).tangent is not None:
+            if grad and t.requires_grad or dual and _forward.unpack_dual(t).tangent is not None:
                 _refuse(what, "no gradients are computed")
-        needed -= 1
     return device
 
 
@@ -115,7 +109,9 @@ def rms_norm_quant(x, weight, eps=1e-6, residual=None, sum_out=None, stream=None
     torch = _torch or _start()
     what = "rms_norm_quant"
     given = (x, weight, residual, sum_out)
-    device = _same_device(what, given, 2)
+    if weight is None:
+        _refuse(what, "the weight is missing")
+    device = _same_device(what, given)
     dtype, shape = x.dtype, x.shape
     code = _types.get(dtype, 3)
     if code == 3:
@@ -164,7 +160,9 @@ def quant_linear(x, x_scale, w, w_scale, bias=None, adapters=None, adapter_ids=N
             _refuse(what, "adapters are three tensors")
         a, b, factor = adapters
     given = (x, x_scale, w, w_scale, bias, a, b, factor, adapter_ids, out)
-    device = _same_device(what, given, 4)
+    if x_scale is None or w is None or w_scale is None:
+        _refuse(what, "the scales and w are needed")
+    device = _same_device(what, given)
     ldx, ldw = _pitch(what, "x", x, torch.int8), _pitch(what, "w", w, torch.int8)
     rows, k = x.shape
     n = w.shape[0]
