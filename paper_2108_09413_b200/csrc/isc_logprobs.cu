@@ -11,12 +11,14 @@
 // out of the second-level cache: every logit not below the k-th maximum is a candidate, usually little more than k of them.
 // Order is by logit, then by lowest index, held as one 64-bit key, so ties are decided exactly.
 //
-// Three forms.  Many rows: persistent blocks, three to an SM, each with a ring of bulk copies that runs on into the next row while the
-// present one's threads join their sums and choose alternatives.  Few rows: a cluster of blocks for a row, joined through
-// its shared memory.  Short rows: a few lanes of a warp, the row in registers.
+// Four forms.  Many long rows: persistent blocks, three to an SM, each with a ring of bulk copies that runs on into the next row while the
+// present one's threads join their sums and choose alternatives (k_log_probs_stream).  Few long rows: a block or a cluster of them for a row, joined through
+// its shared memory (k_log_probs).  Rows of up to 4,096 logits, or 16,384 where there are many: a warp for a row (k_log_probs_warp).  Up to 64: a few lanes of a
+// warp, the row in registers (k_log_probs_group).
 //
-// Memory bound: 2 bytes a logit in bf16, one exponential each (11.6 logits a clock and SM at the copy bandwidth, of 16
-// exponentials); two-number instructions keep the rest below that.
+// What bounds it.  fp32: memory (4,096 x 131,072 with five alternatives 335 us, 98 % of the copy bandwidth).  bf16 has twice the logits a byte and
+// is not: 254 us, 65 %; 218 without alternatives.  Eleven instructions a logit, two numbers in one where that goes, fill 63 % of the issue slots, the
+// exponentials half of their pipe, and with 24 warps an SM what a warp waits for is its own chain of them.
 #include <cuda_runtime.h>
 #include <float.h>
 #include <math.h>

@@ -16,7 +16,8 @@
 // Else a block for a row, a warp for a short one.  Rows too long for registers are read twice.
 //
 // Memory bound: bf16 with a residual 7 bytes an element (reads x and r, writes h and q).  Measured: 16,384 x 8,192 bf16 with residual
-// 158 us, 5.9 TB/s; 8,192 x 4,096 fp32 with residual 80 us, 5.4 TB/s; one row of 4,096 3.6 us.  Two-number instructions, one
+// 155 to 163 us, 5.8 to 6.0 TB/s (249 us for plain Gaussian rows, one in five of them with a doubtful code); 8,192 x 4,096 fp32 with residual 80 us, 5.4 TB/s;
+// one row of 4,096 3.6 us.  Rows at odd addresses (20,000 x 5,001 bf16: 341 us of 107) and beyond registers (4,096 x 20,000: 592 of 88) are far from it.  Two-number instructions, one
 // reciprocal and a hardware maximum over the warp brought the persistent form from 210 us there: what it does between
 // two barriers is what a row costs.
 #include <cuda_runtime.h>

@@ -22,7 +22,7 @@
 // nothing, and what a step loads from memory it waits for); a row that does not share its neighbours' adapter loads its own.
 // kPart, whose rows may each have another adapter: groups of lanes share an output's ranks, straight from memory, while W is on its way.
 //
-// Measured (us; rank 0 is without adapters): 8,192 rows, k = n = 4,096: rank 0 99, 16 132, 32 167, 64 276; k = n = 8,192, rank 32: 502 (410 without: 2.68
+// Measured (us; rank 0 is without adapters): 8,192 rows, k = n = 4,096: rank 0 100, 16 133, 32 159, 64 254; k = n = 8,192, rank 32: 502 (410 without: 2.68
 // POP/s, the rate that the card's power lets cuBLAS's bf16 sustain, twice over); 64 rows, k = 4,096, n = 12,288, 32 adapters of rank 16: 27 (17 without).
 // What bounds it: few rows the copies' start and end around W's bytes; many, the tensor pipe, and from rank 32 on the
 // epilogue's FMAs beside it.
@@ -941,7 +941,7 @@ void plan(LinearParams &p, int n_sms)
     for (int t = least; t <= std::min(4 * least + 4, least + 64); ++t) {
         const int width = ((p.rows + t - 1) / t + 15) & ~15, tiles_n = (p.rows + width - 1) / width;
         // Narrow tiles are bound by W's bytes: two blocks to an SM, so that one's copies run under the other's start and end (16 rows,
-        // k = 8,192, n = 28,672: 49 us with one block and 192 KB of stages, 41 us with two and 80 KB each).
+        // k = 8,192, n = 28,672, no adapters: 49 us with one block and 192 KB of stages, 43 us with two of 96 KB; beside adapters they have 72 KB).
         const bool narrow = width <= 64 && tiles_n == 1;
         const int64_t tiles = (int64_t)p.tiles_m * tiles_n, slots = narrow ? 2 * n_sms : n_sms;
         for (int split = 1; split <= kMostSplit && (split == 1 || (tiles * split <= slots && p.k_blocks >= 4 * split)); split *= 2) {
