@@ -13,11 +13,11 @@
 //
 // Four forms.  Many long rows: persistent blocks, three to an SM, each with a ring of bulk copies that runs on into the next row while the
 // present one's threads join their sums and choose alternatives (k_log_probs_stream).  Few long rows: a block or a cluster of them for a row, joined through
-// its shared memory (k_log_probs).  Rows of up to 4,096 logits, or 16,384 where there are many: a warp for a row (k_log_probs_warp).  Up to 64: a few lanes of a
+// its shared memory (k_log_probs; tiny factors take it too).  Rows of up to 4,096 logits, or 16,384 where there are many: a warp for a row (k_log_probs_warp).  Up to 64: a few lanes of a
 // warp, the row in registers (k_log_probs_group).
 //
 // What bounds it.  fp32: memory (4,096 x 131,072 with five alternatives 335 us, 98 % of the copy bandwidth).  bf16 has twice the logits a byte and
-// is not: 254 us, 65 %; 218 without alternatives.  Eleven instructions a logit, two numbers in one where that goes, fill 63 % of the issue slots, the
+// is not: 257 us, 64 %; 219 without alternatives.  Eleven instructions a logit, two numbers in one where that goes, fill 63 % of the issue slots, the
 // exponentials half of their pipe, and with 24 warps an SM what a warp waits for is its own chain of them.
 #include <cuda_runtime.h>
 #include <float.h>
@@ -25,6 +25,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "isc_ops.cuh"
 #include "isc_ops.h"
@@ -71,22 +72,27 @@ __device__ __forceinline__ float from_ordered(uint32_t o) { return __uint_as_flo
 __device__ __forceinline__ Key make_key(float v, uint32_t index) { return (Key)ordered(v) << 32 | (uint32_t)~index; }
 __device__ __forceinline__ uint32_t key_index(Key k) { return ~(uint32_t)k; }
 
+// (x - m) c.  kFar: also where the difference is beyond single precision's range and a tiny factor brings the two near each other; that of their
+// halves is not, and halving is exact.
+template <bool kFar> __device__ __forceinline__ float times_difference(float x, float m, float c) { return kFar ? fmaf(0.5f, x, -0.5f * m) * (2.0f * c) : (x - m) * c; }
+constexpr float kTinyFactor = 1e-36f;   // from here on such a difference's exponential is zero
+
 // Largest logit, and both sums relative to it in powers of two.
 struct Sums {
     float m, s, u;
-    __device__ __forceinline__ void scale_to(float to, float c)
+    template <bool kFar> __device__ __forceinline__ void scale_to(float to, float c)
     {
-        const float d = fmaxf((m - to) * c, kFloorZ), f = exp2_fast(d);      // (NaN, both infinite: nothing summed yet)
+        const float d = fmaxf(times_difference<kFar>(m, to, c), kFloorZ), f = exp2_fast(d);      // (NaN, both infinite: nothing summed yet)
         u = f * fmaf(d, s, u);
         s *= f;
         m = to;
     }
 };
-__device__ __forceinline__ Sums join(Sums a, Sums b, float c)
+template <bool kFar> __device__ __forceinline__ Sums join(Sums a, Sums b, float c)
 {
     const float m = fmaxf(a.m, b.m);
-    a.scale_to(m, c);
-    b.scale_to(m, c);
+    a.scale_to<kFar>(m, c);
+    b.scale_to<kFar>(m, c);
     return Sums{m, a.s + b.s, a.u + b.u};
 }
 
@@ -107,7 +113,7 @@ __device__ __forceinline__ RowResult row_result(Sums t, bool bad)
 }
 __device__ __forceinline__ float log_prob(const LogProbParams &p, const RowResult &r, float logit)
 {
-    return r.bad ? NAN : r.empty ? -INFINITY : (logit - r.m) * p.scale - r.log_s;
+    return r.bad ? NAN : r.empty ? -INFINITY : times_difference<true>(logit, r.m, p.scale) - r.log_s;
 }
 // A row's given token, loaded ahead of the row: two dependent loads that its end would wait for.
 struct Given { int64_t target; float logit; };
@@ -234,7 +240,7 @@ template <typename T> __device__ __forceinline__ float largest(const Chunk<T> &e
 }
 
 // A thread's part of a row.  Sums are kept as pairs, relative to m.
-struct Own {
+template <bool kFar> struct Own {
     float m = -INFINITY, seen = -INFINITY;      // seen: m, or NaN if there is one
     Pair s = 0, u = 0;
     float top = -INFINITY;              // of the present subset of its chunks: the largest logit,
@@ -256,7 +262,7 @@ struct Own {
     __device__ __forceinline__ void rise(float to, float c)
     {
         Sums all = sums();
-        all.scale_to(to, c);
+        all.scale_to<kFar>(to, c);
         m = to;
         s = make_pair(all.s, 0.0f);
         u = make_pair(all.u, 0.0f);
@@ -281,7 +287,7 @@ struct Own {
     {
         float sum = 0.0f, weighted = 0.0f;
         for (int j = 0; j < Chunk<T>::kSize; ++j) {
-            const float z = fmaxf((to_float(e.v[j]) - m) * c, kFloorZ), ez = exp2_fast(z);
+            const float z = fmaxf(times_difference<kFar>(to_float(e.v[j]), m, c), kFloorZ), ez = exp2_fast(z);
             sum += ez;
             weighted = fmaf(ez, z, weighted);
         }
@@ -371,21 +377,21 @@ __device__ __forceinline__ uint32_t read_remote(uint32_t addr)
 }
 
 // Every thread gets its team's sums.  `edge`: this thread's logit outside the chunks (minus infinity: none).
-template <int kWarps, int kSubsets> __device__ __forceinline__ Sums join_all(Shared<kWarps, kSubsets> &sh, const Team &team, const Own &own, float edge, float c, bool &bad)
+template <bool kFar, int kWarps, int kSubsets> __device__ __forceinline__ Sums join_all(Shared<kWarps, kSubsets> &sh, const Team &team, const Own<kFar> &own, float edge, float c, bool &bad)
 {
     Sums all = own.sums();
-    if (edge > -INFINITY) all = join(all, Sums{edge, 1.0f, 0.0f}, c);
+    if (edge > -INFINITY) all = join<kFar>(all, Sums{edge, 1.0f, 0.0f}, c);
     bad = !(own.seen < INFINITY) || edge != edge || edge == INFINITY;
 #pragma unroll
     for (int d = 16; d; d >>= 1)
-        all = join(all, Sums{__shfl_xor_sync(0xffffffffu, all.m, d), __shfl_xor_sync(0xffffffffu, all.s, d), __shfl_xor_sync(0xffffffffu, all.u, d)}, c);
+        all = join<kFar>(all, Sums{__shfl_xor_sync(0xffffffffu, all.m, d), __shfl_xor_sync(0xffffffffu, all.s, d), __shfl_xor_sync(0xffffffffu, all.u, d)}, c);
     bad = __any_sync(0xffffffffu, bad) != 0;
     if ((team.t & 31) == 0) { sh.warp[team.t >> 5] = all; sh.bad[team.t >> 5] = bad; }
     if (team.t == 0) sh.n_candidates = 0;
     team.sync();
     all = sh.warp[0];
     bad = sh.bad[0] != 0;
-    for (int w = 1; w < team.threads >> 5; ++w) { all = join(all, sh.warp[w], c); bad |= sh.bad[w] != 0; }
+    for (int w = 1; w < team.threads >> 5; ++w) { all = join<kFar>(all, sh.warp[w], c); bad |= sh.bad[w] != 0; }
     return all;
 }
 
@@ -523,8 +529,8 @@ template <int kWarps, int kSubsets> __device__ __forceinline__ void write_result
     if (p.votes && t == 0 && !bad && sh.top[0]) atomicAdd(p.votes + key_index(sh.top[0]), 1);
 }
 
-// few rows: a block or a cluster of them for a row
-template <typename T> __global__ void __launch_bounds__(kThreads) k_log_probs(const __grid_constant__ LogProbParams p)
+// few rows: a block or a cluster of them for a row.  kFar: tiny factors, any number of rows
+template <typename T, bool kFar> __global__ void __launch_bounds__(kThreads) k_log_probs(const __grid_constant__ LogProbParams p)
 {
     __shared__ Shared<kThreads / 32> sh;
     const Team team{(int)threadIdx.x, (int)blockDim.x, 0};
@@ -534,7 +540,7 @@ template <typename T> __global__ void __launch_bounds__(kThreads) k_log_probs(co
     const int stride = threads * p.cluster, first = rank * threads + t, edge_index = rank == 0 && t < 32 ? row.edge(t) : -1;
     const float c = p.scale2, edge = edge_index >= 0 ? to_float(row.at[edge_index]) : -INFINITY;
     const Given given = given_of(p, row.at, row_index, rank == 0 && t == 0);
-    Own own;
+    Own<kFar> own;
     constexpr int kAhead = 4;
     for (int i0 = first; i0 < row.chunks; i0 += kAhead * stride) {
         Chunk<T> e[kAhead];
@@ -554,7 +560,7 @@ template <typename T> __global__ void __launch_bounds__(kThreads) k_log_probs(co
         if (rank == 0) {
             for (int b = 1; t < 32 && b < p.cluster; ++b) {      // the first warp writes the results
                 const uint32_t from = in_block(&sh.block, b);
-                all = join(all, Sums{__uint_as_float(read_remote(from)), __uint_as_float(read_remote(from + 4)), __uint_as_float(read_remote(from + 8))}, c);
+                all = join<kFar>(all, Sums{__uint_as_float(read_remote(from)), __uint_as_float(read_remote(from + 4)), __uint_as_float(read_remote(from + 8))}, c);
                 bad |= read_remote(in_block(&sh.block_bad, b)) != 0;
             }
             if (k) {
@@ -594,7 +600,7 @@ template <typename T> __global__ void __launch_bounds__(32 * kRowWarps) k_log_pr
     const int edge_index = row.edge(t);
     const float edge = edge_index >= 0 ? to_float(row.at[edge_index]) : -INFINITY;
     const Given given = given_of(p, row.at, r, t == 0);
-    Own own;
+    Own<false> own;
     constexpr int kAhead = 4;
     for (int i0 = t; i0 < row.chunks; i0 += 32 * kAhead) {
         Chunk<T> e[kAhead];
@@ -659,7 +665,7 @@ template <typename T> __global__ void __launch_bounds__(kStreamThreads + 32, kSt
         const int edge_index = t < 32 ? row.edge(t) : -1;
         const float edge = edge_index >= 0 ? to_float(row.at[edge_index]) : -INFINITY;
         const Given given = given_of(p, row.at, r, t == 0);
-        Own own;
+        Own<false> own;
         // two subsets a thread: what is read again for the alternatives is half.  Their keys wait where the candidates will be: there
         // are no registers for them
         const int n_pieces = (row.chunks + kPieceChunks - 1) / kPieceChunks, per_subset = (n_pieces + kStreamSubsets - 1) / kStreamSubsets, each = per_subset * (kPieceChunks / kStreamThreads);
@@ -733,7 +739,7 @@ template <typename T, int kLanes, int kHeld> __global__ void __launch_bounds__(k
         if (m > -INFINITY && !bad) {
 #pragma unroll
             for (int e = 0; e < kHeld; ++e) {
-                const float z = fmaxf((x[e] - m) * c, kFloorZ), ez = exp2_fast(z);
+                const float z = fmaxf(times_difference<true>(x[e], m, c), kFloorZ), ez = exp2_fast(z);
                 all.s += ez;
                 all.u = fmaf(ez, z, all.u);
             }
@@ -798,12 +804,15 @@ template <typename T> cudaError_t launch_log_probs(const Device &dev, LogProbPar
         else k_log_probs_group<T, 8, 8><<<grid, kGroupThreads, 0, st>>>(p);
         return cudaGetLastError();
     }
+    // Factors so small that logits further apart than single precision's range weigh something: one form for all rows, with the arithmetic for
+    // that, so that the others need none (in them it cost 2 % of a long row).  fp16 and int8 have no such logits.
+    const bool far = p.scale2 < kTinyFactor && (std::is_same<T, float>::value || std::is_same<T, __nv_bfloat16>::value);
     // (a warp takes 16 chunks a lane in the time that a block's barriers take)
-    if (p.vocab <= 4096 || (p.vocab <= 16384 && p.rows >= 16 * dev.n_sms)) {
+    if (!far && (p.vocab <= 4096 || (p.vocab <= 16384 && p.rows >= 16 * dev.n_sms))) {
         k_log_probs_warp<T><<<(unsigned)((p.rows + kRowWarps - 1) / kRowWarps), 32 * kRowWarps, 0, st>>>(p);
         return cudaGetLastError();
     }
-    if (p.rows >= 2 * kStreamBlocks * dev.n_sms) {
+    if (!far && p.rows >= 2 * kStreamBlocks * dev.n_sms) {
         const cudaError_t e = cudaFuncSetAttribute(k_log_probs_stream<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, kPieces * kPieceBytes);
         if (e != cudaSuccess) return e;
         k_log_probs_stream<T><<<(unsigned)(kStreamBlocks * dev.n_sms), kStreamThreads + 32, kPieces * kPieceBytes, st>>>(p);
@@ -824,7 +833,9 @@ template <typename T> cudaError_t launch_log_probs(const Device &dev, LogProbPar
     cfg.stream = st;
     cfg.attrs = &attr;
     cfg.numAttrs = p.cluster > 1 ? 1 : 0;
-    return cudaLaunchKernelEx(&cfg, k_log_probs<T>, p);
+    if constexpr (std::is_same<T, float>::value || std::is_same<T, __nv_bfloat16>::value)
+        if (far) return cudaLaunchKernelEx(&cfg, k_log_probs<T, true>, p);
+    return cudaLaunchKernelEx(&cfg, k_log_probs<T, false>, p);
 }
 
 }  // namespace
